@@ -51,6 +51,8 @@
  *     writes a status word into the workspace and the compute kernels then
  *     write nothing; bs_read_device_status() reports it.
  *   - Calls that share a workspace must be ordered on one stream.
+ * bs_qkv.h declares the operators around this attention: the norm and rotation of queries and keys,
+ * and a paged key/value cache.
  */
 #ifndef BS_ATTN_H
 #define BS_ATTN_H
@@ -345,7 +347,10 @@ enum {
   BS_KERNEL_FINALIZE = 5,   /* float32 dQ accumulator or workspace -> dq */
   BS_KERNEL_MERGE = 6,      /* LSE merge */
   BS_KERNEL_XENT = 7,       /* softmax cross-entropy */
-  BS_KERNEL_COUNT = 8
+  BS_KERNEL_QK_ROPE = 8,    /* norm and rotation of queries and keys, both directions (bs_qkv.h) */
+  BS_KERNEL_KV_APPEND = 9,  /* append to a paged cache (bs_qkv.h) */
+  BS_KERNEL_PAGED = 10,     /* attention over a paged cache, with the merge of its parts (bs_qkv.h) */
+  BS_KERNEL_COUNT = 11
 };
 
 /* Profiling (off by default, process-wide).  While enabled, every call

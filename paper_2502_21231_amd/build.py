@@ -21,7 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libbs_attn.so")
 
 SOURCES = ["plan.hip", "fwd_bf16.hip", "few_bf16.hip", "dq_bf16.hip", "dkdv_bf16.hip", "f32.hip", "rowwise.hip",
-           "xent.hip", "capi.hip"]
+           "xent.hip", "qkv.hip", "paged.hip", "capi.hip", "capi_qkv.hip"]
 # per-source additions: the dQ kernel's loop schedules faster under the backend's max-ILP
 # strategy (the forward's and dK/dV's do not)
 SOURCE_FLAGS = {"dq_bf16.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]}

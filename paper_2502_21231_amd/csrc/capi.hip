@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "attn.hpp"
+#include "capi.hpp"
 
 // Scratch of the allocation-free forward (bs_attn_varlen_fwd_noalloc): the plan that the
 // forward kernel walks (header, per-segment offsets, work list), then the pieces of the
@@ -22,8 +23,8 @@ static __device__ __align__(256) unsigned char scratch[kNoAllocScratchBytes + kF
 
 namespace bs {
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
 
 int fail(int code, const char* fmt, ...) {
   va_list ap;
@@ -42,9 +43,7 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(BS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-constexpr int64_t kMaxTokens = int64_t(1) << 30;
-// query heads: keeps the byte offsets inside one tile of rows below 2^31
-constexpr int32_t kMaxHeads = 4096;
+namespace {
 
 // Profiling: pairs of HIP events recorded around each kernel launch while enabled.
 struct Profiler {
@@ -79,35 +78,61 @@ void give_back(hipEvent_t e) {
   P.spare.push_back(e);
 }
 
-// Records an event pair around the launches made during its lifetime (none when an event
-// cannot be had: the one that was is returned to the pool).
-class ProfScope {
- public:
-  ProfScope(int kind, hipStream_t s) : kind_(kind), s_(s) {
-    if (!prof().on.load(std::memory_order_relaxed)) return;
-    a_ = take_event();
-    b_ = take_event();
-    if (a_ && b_) {
-      hipEventRecord(a_, s_);
-    } else {
-      give_back(a_);
-      give_back(b_);
-      a_ = b_ = nullptr;
-    }
-  }
-  ~ProfScope() {
-    if (!a_ || !b_) return;
-    hipEventRecord(b_, s_);
-    Profiler& P = prof();
-    std::lock_guard<std::mutex> g(P.mu);
-    P.recs[kind_].emplace_back(a_, b_);
-  }
+}  // namespace
 
- private:
-  int kind_;
-  hipStream_t s_;
-  hipEvent_t a_ = nullptr, b_ = nullptr;
-};
+ProfScope::ProfScope(int kind, hipStream_t s) : kind_(kind), s_(s) {
+  if (!prof().on.load(std::memory_order_relaxed)) return;
+  a_ = take_event();
+  b_ = take_event();
+  if (a_ && b_) {
+    hipEventRecord(a_, s_);
+  } else {
+    give_back(a_);
+    give_back(b_);
+    a_ = b_ = nullptr;
+  }
+}
+ProfScope::~ProfScope() {
+  if (!a_ || !b_) return;
+  hipEventRecord(b_, s_);
+  Profiler& P = prof();
+  std::lock_guard<std::mutex> g(P.mu);
+  P.recs[kind_].emplace_back(a_, b_);
+}
+
+int check_dims(const bs_dims* d, bool need_kv) {
+  if (d == nullptr) return fail(BS_ERR_INVALID_ARG, "dims is NULL");
+  if (d->dtype != BS_F32 && d->dtype != BS_BF16)
+    return fail(BS_ERR_UNSUPPORTED, "dtype %d is not BS_F32 or BS_BF16", d->dtype);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(BS_ERR_UNSUPPORTED, "head_dim %d is not 64 or 128", d->head_dim);
+  if (d->hq < 1 || d->hq > kMaxHeads)
+    return fail(BS_ERR_INVALID_ARG, "hq = %d out of [1, %d]", d->hq, kMaxHeads);
+  if (d->total_q < 0 || d->total_q >= kMaxTokens)
+    return fail(BS_ERR_INVALID_ARG, "total_q = %lld out of [0, 2^30)", (long long)d->total_q);
+  if (need_kv) {
+    if (d->hkv < 1 || d->hq % d->hkv != 0)
+      return fail(BS_ERR_INVALID_ARG, "hq = %d must be a positive multiple of hkv = %d", d->hq, d->hkv);
+    if (d->total_k < 0 || d->total_k >= kMaxTokens)
+      return fail(BS_ERR_INVALID_ARG, "total_k = %lld out of [0, 2^30)", (long long)d->total_k);
+  }
+  return BS_OK;
+}
+
+int check_ptr(const void* p, int64_t count, const char* name) {
+  if (count == 0) return BS_OK;
+  if (p == nullptr) return fail(BS_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
+    return fail(BS_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+  return BS_OK;
+}
+
+int check_scale(float s) {
+  if (!isfinite(s) || !(s > 0.f)) return fail(BS_ERR_INVALID_ARG, "scale must be finite and > 0");
+  return BS_OK;
+}
+
+namespace {
 
 struct PlanCfg {
   PlanKind kind;
@@ -145,38 +170,6 @@ int plans_of(int op, const bs_dims& d, PlanCfg out[2]) {
 int64_t max_items_of(const PlanCfg& c, const bs_dims& d, int64_t nseg, bool varlen) {
   const int64_t ta = c.kind == kPlanFwd ? d.total_q : d.total_k;
   return (ta + c.tile_a - 1) / c.tile_a + (varlen ? nseg : 0);
-}
-
-int check_dims(const bs_dims* d, bool need_kv) {
-  if (d == nullptr) return fail(BS_ERR_INVALID_ARG, "dims is NULL");
-  if (d->dtype != BS_F32 && d->dtype != BS_BF16)
-    return fail(BS_ERR_UNSUPPORTED, "dtype %d is not BS_F32 or BS_BF16", d->dtype);
-  if (d->head_dim != 64 && d->head_dim != 128)
-    return fail(BS_ERR_UNSUPPORTED, "head_dim %d is not 64 or 128", d->head_dim);
-  if (d->hq < 1 || d->hq > kMaxHeads)
-    return fail(BS_ERR_INVALID_ARG, "hq = %d out of [1, %d]", d->hq, kMaxHeads);
-  if (d->total_q < 0 || d->total_q >= kMaxTokens)
-    return fail(BS_ERR_INVALID_ARG, "total_q = %lld out of [0, 2^30)", (long long)d->total_q);
-  if (need_kv) {
-    if (d->hkv < 1 || d->hq % d->hkv != 0)
-      return fail(BS_ERR_INVALID_ARG, "hq = %d must be a positive multiple of hkv = %d", d->hq, d->hkv);
-    if (d->total_k < 0 || d->total_k >= kMaxTokens)
-      return fail(BS_ERR_INVALID_ARG, "total_k = %lld out of [0, 2^30)", (long long)d->total_k);
-  }
-  return BS_OK;
-}
-
-int check_ptr(const void* p, int64_t count, const char* name) {
-  if (count == 0) return BS_OK;
-  if (p == nullptr) return fail(BS_ERR_INVALID_ARG, "%s is NULL", name);
-  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
-    return fail(BS_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-  return BS_OK;
-}
-
-int check_scale(float s) {
-  if (!isfinite(s) || !(s > 0.f)) return fail(BS_ERR_INVALID_ARG, "scale must be finite and > 0");
-  return BS_OK;
 }
 
 // How a bf16 kernel of few workgroups runs: by its own plan (no list), each work item's chain of
@@ -480,23 +473,6 @@ int check_varlen_args(int op, const int32_t* cu_q, const int32_t* cu_k, const in
   if (is_packed(op) && num_seqs > 0 && (q_pos == nullptr || k_pos == nullptr))
     return fail(BS_ERR_INVALID_ARG, "q_pos / k_pos is NULL");
   return BS_OK;
-}
-
-#define BS_TRY(x)                 \
-  do {                            \
-    int rc__ = (x);               \
-    if (rc__ != BS_OK) return rc__; \
-  } while (0)
-#define BS_HIP(x, what)                        \
-  do {                                         \
-    hipError_t e__ = (x);                      \
-    if (e__ != hipSuccess) return hip_fail(e__, what); \
-  } while (0)
-
-// True when the byte ranges [a, a + na) and [b, b + nb) intersect.
-bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
 // merge == NULL: writes the step's (out, lse).  Otherwise folds the step into the

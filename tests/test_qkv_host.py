@@ -1,0 +1,181 @@
+"""Host-side checks of the entry points of bs_qkv.h that need no GPU: every declared function is exported
+and bound, and bad arguments are refused before anything is enqueued."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2502_21231_amd import bs_attn as B
+from paper_2502_21231_amd import bs_qkv as Q
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 1 << 40  # non-null, aligned, never used
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        pytest.fail("libbs_attn.so is not built (run __graft_entry__.build())")
+    return Q._library()
+
+
+def test_exports_every_declared_symbol(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "bs_qkv.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(bs_\w+)\s*\(", text))
+    assert names == set(Q.EXPORTS)
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+def dims(**kw):
+    d = dict(total_q=128, total_k=0, hq=4, hkv=2, head_dim=128, dtype=B.BS_BF16)
+    d.update(kw)
+    return B.bs_dims(**d)
+
+
+def params(**kw):
+    d = dict(inv_freq=FAKE, rot_dim=128, interleaved=0, q_weight=FAKE, k_weight=FAKE, weight_dtype=B.BS_F32, eps=1e-6)
+    d.update(kw)
+    return Q.bs_qk_params(**d)
+
+
+def cache(**kw):
+    d = dict(k=FAKE, v=FAKE + (1 << 30), num_pages=8, page_stride=4096, token_stride=256, head_stride=128,
+             block_table=FAKE, table_stride=4, max_pages=4, page_size=16, kv_lens=FAKE)
+    d.update(kw)
+    return Q.bs_paged_cache(**d)
+
+
+Q_AT, K_AT, QO_AT, KO_AT = (FAKE + (i << 32) for i in range(2, 6))
+
+
+def fwd(lib, d=None, p=None, q=Q_AT, qs=512, k=K_AT, ks=256, pos=FAKE, qo=QO_AT, ko=KO_AT):
+    d, p = d or dims(), p or params()
+    return lib.bs_qk_norm_rope_fwd(ctypes.byref(d), ctypes.byref(p), q, qs, k, ks, pos, qo, ko, None)
+
+
+def said(code, rc, word):
+    assert rc == code and word in B.bs_last_error(), (rc, B.bs_last_error())
+
+
+BAD, UNS, WS = B.BS_ERR_INVALID_ARG, B.BS_ERR_UNSUPPORTED, B.BS_ERR_WORKSPACE
+
+
+def test_norm_rope_refusals(lib):
+    said(UNS, fwd(lib, dims(head_dim=96)), "head_dim")
+    said(UNS, fwd(lib, dims(dtype=3)), "dtype")
+    said(BAD, fwd(lib, dims(hq=3)), "multiple of hkv")
+    said(BAD, fwd(lib, dims(total_q=-1)), "total_q")
+    for rot in (-16, 8, 24, 144):
+        said(BAD, fwd(lib, p=params(rot_dim=rot)), "rot_dim")
+    said(BAD, fwd(lib, p=params(inv_freq=None)), "inv_freq")
+    said(BAD, fwd(lib, p=params(inv_freq=FAKE + 2)), "inv_freq")
+    said(UNS, fwd(lib, p=params(weight_dtype=7)), "weight_dtype")
+    said(BAD, fwd(lib, p=params(q_weight=FAKE + 2)), "weight")
+    said(BAD, fwd(lib, p=params(eps=float("nan"))), "eps")
+    said(BAD, fwd(lib, p=params(eps=-1.0)), "eps")
+    said(BAD, fwd(lib, q=None), "q is NULL")
+    said(BAD, fwd(lib, k=K_AT + 8), "k is not 16-byte aligned")
+    said(BAD, fwd(lib, qs=511), "stride of q")
+    said(BAD, fwd(lib, qs=516), "stride of q")
+    said(BAD, fwd(lib, ks=128), "stride of k")
+    said(BAD, fwd(lib, pos=None), "positions")
+    said(BAD, fwd(lib, pos=FAKE + 4), "positions")
+    said(BAD, fwd(lib, qo=None), "q_out is NULL")
+    said(BAD, fwd(lib, qo=Q_AT + 1024), "q_out overlaps q")
+    said(BAD, fwd(lib, qo=Q_AT, qs=1024), "q_out overlaps q")  # equal pointers, another stride
+    said(BAD, fwd(lib, ko=QO_AT + 256), "q_out overlaps k_out")
+    said(BAD, fwd(lib, ko=Q_AT + 256), "k_out overlaps q")
+    assert lib.bs_qk_norm_rope_workspace_size(ctypes.byref(dims(head_dim=100))) == 0
+    assert lib.bs_qk_norm_rope_workspace_size(ctypes.byref(dims())) > 0
+    # nothing to do: nothing enqueued
+    assert fwd(lib, dims(total_q=0), q=None, k=None, pos=None, qo=None, ko=None) == B.BS_OK
+
+
+def bwd(lib, d=None, p=None, q=Q_AT, gq=QO_AT, gk=KO_AT, dq=FAKE + (7 << 32), dqs=1024, dk=FAKE + (7 << 32) + 1024,
+        dks=1024, wq=FAKE, wk=FAKE, ws=FAKE, ws_bytes=1 << 30):
+    d, p = d or dims(), p or params()
+    return lib.bs_qk_norm_rope_bwd(ctypes.byref(d), ctypes.byref(p), q, 512, K_AT, 256, FAKE, gq, gk, dq, dqs, dk, dks,
+                                   wq, wk, ws, ws_bytes, None)
+
+
+def test_norm_rope_backward_refusals(lib):
+    said(BAD, bwd(lib, q=None), "q is NULL")
+    said(BAD, bwd(lib, gq=None), "dq_out is NULL")
+    said(BAD, bwd(lib, dk=FAKE + (7 << 32) + 512), "dq overlaps dk")  # rows of one buffer that cross
+    said(BAD, bwd(lib, dq=Q_AT + 16, dqs=512), "dq overlaps q")
+    said(BAD, bwd(lib, dk=QO_AT), "dk overlaps dq_out")
+    said(BAD, bwd(lib, p=params(q_weight=None)), "weight that is NULL")
+    said(WS, bwd(lib, ws=None), "workspace")
+    said(WS, bwd(lib, ws=FAKE + 16), "workspace")
+    said(WS, bwd(lib, ws_bytes=64), "smaller")
+    said(BAD, bwd(lib, wq=FAKE + 2), "dq_weight")
+
+
+def append(lib, d=None, p=None, c=None, cu=FAKE, n=2, q=Q_AT, qs=512, k=K_AT, ks=256, v=FAKE + (8 << 32), vs=256,
+           qo=QO_AT):
+    d, p, c = d or dims(), p or params(), c or cache()
+    return lib.bs_kv_append(ctypes.byref(d), ctypes.byref(p), ctypes.byref(c), cu, n, q, qs, k, ks, v, vs, qo, None)
+
+
+def test_append_and_cache_refusals(lib):
+    for kw, code, word in ((dict(num_pages=0), BAD, "num_pages"), (dict(num_pages=1 << 31), BAD, "num_pages"),
+                           (dict(page_size=8), UNS, "page_size"), (dict(page_size=48), UNS, "page_size"),
+                           (dict(page_size=8192), UNS, "page_size"), (dict(page_stride=0), BAD, "strides"),
+                           (dict(token_stride=-256), BAD, "strides"), (dict(head_stride=132), BAD, "strides"),
+                           (dict(token_stride=1 << 26), UNS, "token_stride"),
+                           (dict(page_stride=1 << 62), BAD, "address range"),
+                           (dict(k=None), BAD, "cache k is NULL"), (dict(v=FAKE + 8), BAD, "cache v"),
+                           (dict(max_pages=5), BAD, "max_pages"), (dict(max_pages=-1), BAD, "max_pages"),
+                           (dict(block_table=None), BAD, "block_table"), (dict(kv_lens=None), BAD, "kv_lens"),
+                           (dict(kv_lens=FAKE + 2), BAD, "aligned")):
+        said(code, append(lib, c=cache(**kw)), word)
+        said(code, paged(lib, c=cache(**kw)), word)
+    said(BAD, append(lib, cu=None), "cu_seqlens")
+    said(BAD, append(lib, cu=FAKE + 1), "cu_seqlens")
+    said(BAD, append(lib, n=-1), "num_seqs")
+    said(BAD, append(lib, k=None), "k is NULL")
+    said(BAD, append(lib, vs=128), "stride of v")
+    said(BAD, append(lib, qo=None), "q_out is NULL")
+    said(BAD, append(lib, qo=K_AT), "q_out overlaps k")
+    said(BAD, append(lib, k=FAKE + 512), "k overlaps the cache")
+    said(BAD, append(lib, p=params(rot_dim=20)), "rot_dim")
+
+
+def paged(lib, d=None, c=None, q=Q_AT, cu=FAKE, n=2, most=64, scale=0.1, out=QO_AT, lse=FAKE, ws=FAKE,
+          ws_bytes=1 << 30):
+    d, c = d or dims(), c or cache()
+    return lib.bs_attn_paged_fwd(ctypes.byref(d), q, ctypes.byref(c), cu, n, most, 1, scale, out, lse, ws, ws_bytes, None)
+
+
+def test_paged_attention_refusals(lib):
+    said(UNS, paged(lib, n=16385), "num_seqs")
+    said(BAD, paged(lib, n=-1), "num_seqs")
+    said(BAD, paged(lib, most=-1), "max_seqlen_k")
+    said(BAD, paged(lib, most=1 << 30), "max_seqlen_k")
+    said(BAD, paged(lib, scale=0.0), "scale")
+    said(BAD, paged(lib, out=None), "out is NULL")
+    said(BAD, paged(lib, out=Q_AT), "out overlaps q")
+    said(BAD, paged(lib, out=FAKE + 256), "out overlaps the cache")
+    said(BAD, paged(lib, lse=None), "lse is NULL")
+    said(WS, paged(lib, ws=None), "workspace")
+    said(WS, paged(lib, ws=FAKE + 128), "workspace")
+    said(WS, paged(lib, ws_bytes=100), "smaller")
+    size = lib.bs_attn_paged_workspace_size
+    assert size(ctypes.byref(dims()), 2, 64) > 0
+    assert size(ctypes.byref(dims()), -1, 64) == 0 and size(ctypes.byref(dims(hq=5)), 2, 64) == 0
+
+
+def test_binding_refuses_tensors_on_the_host():
+    x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="on the GPU"):
+        Q.bs_qk_norm_rope_fwd(x, x, torch.zeros(4, dtype=torch.int64), Q.make_qk_params())
+    with pytest.raises(ValueError, match="on the GPU"):
+        Q.make_qk_params(inv_freq=torch.zeros(8))
+    pages = torch.zeros(3, 16, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="on the GPU"):
+        Q.make_paged_cache(pages, pages, torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(ValueError, match="page_size"):
+        Q.make_paged_cache(x, x, None, None)
