@@ -106,7 +106,7 @@ size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32
  * contiguous; writes out [T, hq, head_dim] and lse [hq, T]; a row that sees no key gets out = 0,
  * lse = -inf.  Rows from cu_seqlens_q[num_seqs] on are left as they were.  What the pages hold behind
  * a sequence's last token is not looked at (it may be NaN).
- *   - max_seqlen_k bounds kv_lens.  num_seqs is at most 16,384.
+ *   - max_seqlen_k (below 2^30) bounds kv_lens.  num_seqs is at most 16,384, T hq below 2^31.
  *   - cu_seqlens_q and kv_lens are checked on the device: first entry not 0, a negative length, more
  *     rows than T, kv_lens beyond max_seqlen_k or the table give a status (BS_DEV_BAD_FIRST,
  *     BS_DEV_NOT_MONOTONE, BS_DEV_BAD_TOTAL, BS_DEV_TOO_LONG) that bs_read_device_status(workspace)

@@ -124,7 +124,8 @@ int check_paged(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k) {
   if (num_seqs > kPagedMaxSeqs)
     return fail(BS_ERR_UNSUPPORTED, "num_seqs = %d is above %d", num_seqs, kPagedMaxSeqs);
   if (max_seqlen_k >= kMaxTokens) return fail(BS_ERR_INVALID_ARG, "max_seqlen_k = %d is not below 2^30", max_seqlen_k);
-  (void)d;
+  if (d.total_q * d.hq > INT32_MAX)
+    return fail(BS_ERR_UNSUPPORTED, "total_q * hq = %lld is not below 2^31", (long long)(d.total_q * d.hq));
   return BS_OK;
 }
 

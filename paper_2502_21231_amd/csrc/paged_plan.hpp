@@ -1,0 +1,95 @@
+// How the work of a paged attention call is shared, as plain functions for host and device.
+//
+// A segment's rows (lq queries x the `group` heads of a KV head) form blocks of BM; row block i sees
+// the first keys(i) keys, in v(i) blocks of BLK, at least one.  All blocks of all row blocks, segments and
+// KV heads form one line that is cut into equal ranges, one per workgroup, so that a workgroup's
+// range may begin and end inside a row block, whatever the lengths.
+//
+// With a causal mask v(i) grows with i, and its sum has no closed form because of the rounding.  The
+// line therefore gives row block i the slots [S(i), S(i + 1)) of
+//   S(i) = floor(i (A + i B)),  A + B (2 i + 1) >= v(i) + 1 / BLK,
+// a sum of the unrounded counts: S(i + 1) - S(i) >= floor(A + B (2 i + 1)) >= v(i), about one slot
+// more than needed on average.  The slots behind the v(i)-th are skipped.  The one row block of a
+// short segment has its v exactly.
+#pragma once
+
+#include <stdint.h>
+
+#if defined(__HIP__)
+#define BS_HD __host__ __device__ __forceinline__
+#else
+#define BS_HD inline
+#endif
+
+namespace bs {
+
+struct PagedSeg {
+  int32_t lq, lk, group, causal;
+};
+
+BS_HD int32_t paged_row_blocks(const PagedSeg& s, int BM) {
+  return (int32_t)(((int64_t)s.lq * s.group + BM - 1) / BM);
+}
+
+// Keys that some row of block i sees, and their blocks.
+BS_HD int32_t paged_keys(const PagedSeg& s, int BM, int32_t i) {
+  if (!s.causal) return s.lk;
+  const uint32_t last = ((uint32_t)(i + 1) * (uint32_t)BM - 1) / (uint32_t)s.group;
+  const int32_t q = last < (uint32_t)s.lq ? (int32_t)last : s.lq - 1;
+  const int32_t k = s.lk - s.lq + q + 1;  // at most lk
+  return k > 0 ? k : 0;
+}
+BS_HD int32_t paged_blocks(const PagedSeg& s, int BM, int BLK, int32_t i) {
+  const int32_t k = paged_keys(s, BM, i);
+  return k > BLK ? (k + BLK - 1) / BLK : 1;
+}
+
+// The slots of a segment.
+struct PagedCost {
+  double a, b;
+  int32_t n;  // row blocks
+  // (a product of one rounding, so that every caller gets the same number)
+  BS_HD int64_t start(int32_t i) const { return (int64_t)__builtin_floor(i * __builtin_fma((double)i, b, a)); }
+  // The row block that slot y of the segment belongs to.
+  BS_HD int32_t find(int64_t y) const {
+    double g = b > 0 ? (__builtin_sqrt(a * a + 4 * b * (double)y) - a) / (2 * b) : (double)y / a;
+    int32_t i = g < n ? (int32_t)g : n - 1;
+    while (i > 0 && start(i) > y) --i;
+    while (i + 1 < n && start(i + 1) <= y) ++i;
+    return i;
+  }
+};
+BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
+  PagedCost c;
+  c.n = paged_row_blocks(s, BM);
+  c.b = 0;
+  c.a = s.lk > BLK ? (s.lk + BLK - 1) / BLK : 1;
+  if (s.causal && c.n > 1) {
+    const double step = (double)BM / s.group / BLK;
+    const int32_t first = s.lk - s.lq + 1;
+    c.b = step * 0.5;
+    c.a = (double)((first > 0 ? first : 0) + BLK) / BLK + c.b;
+  }
+  return c;
+}
+
+// Workgroups' ranges of a line of `all` slots: `per` slots each, `active` of them not empty.
+struct PagedRanges {
+  int64_t all, per;
+  int32_t active;
+};
+BS_HD PagedRanges paged_ranges(int64_t all, int32_t grid) {
+  PagedRanges r;
+  r.all = all;
+  r.per = all > grid ? (all + grid - 1) / grid : 1;
+  r.active = (int32_t)((all + r.per - 1) / r.per);
+  return r;
+}
+// Range of block b of the grid: blocks are dealt to the 8 XCDs in turn, and each XCD takes neighbouring
+// ranges, which read the same keys.  -1: none.
+BS_HD int32_t paged_range_of(int32_t b, int32_t active) {
+  const int32_t each = (active + 7) >> 3, at = b >> 3, w = (b & 7) * each + at;
+  return at < each && w < active ? w : -1;
+}
+
+}  // namespace bs

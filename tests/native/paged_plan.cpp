@@ -1,0 +1,107 @@
+// The line of a paged attention call (csrc/paged_plan.hpp), walked on the host: every key block of
+// every row block is taken by exactly one range, the ranges of a shared row block follow one another, and
+// every row of a block sees no key behind its blocks.
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <set>
+#include <vector>
+
+#include "../../paper_2502_21231_amd/csrc/paged_plan.hpp"
+
+using namespace bs;
+
+#define CHECK(c)                                                     \
+  do {                                                               \
+    if (!(c)) {                                                      \
+      std::fprintf(stderr, "line %d: %s\n", __LINE__, #c);           \
+      std::exit(1);                                                  \
+    }                                                                \
+  } while (0)
+
+static void segment(const PagedSeg& s, int BM, int BLK) {
+  const PagedCost c = paged_cost(s, BM, BLK);
+  CHECK(c.n == paged_row_blocks(s, BM));
+  CHECK(c.start(0) == 0);
+  int64_t need = 0;
+  for (int32_t i = 0; i < c.n; ++i) {
+    const int32_t v = paged_blocks(s, BM, BLK, i);
+    const int64_t at = c.start(i), room = c.start(i + 1) - at;
+    need += v;
+    CHECK(v >= 1 && room >= v && room <= v + 2 + (s.lk < s.lq ? s.lq / BLK + 1 : 0) + BM / BLK + 1);
+    CHECK(c.find(at) == i && c.find(at + room - 1) == i && c.find(at + room / 2) == i);
+    // the keys of the block's last row, by the definition
+    const int64_t last = std::min<int64_t>((int64_t)s.lq * s.group, (int64_t)(i + 1) * BM) - 1;
+    const int64_t seen = s.causal ? std::min<int64_t>(s.lk, std::max<int64_t>(0, s.lk - s.lq + last / s.group + 1)) : s.lk;
+    CHECK(paged_keys(s, BM, i) == seen);
+    CHECK((int64_t)v * BLK >= seen && (v == 1 || (int64_t)(v - 1) * BLK < seen));
+  }
+  if (c.n == 1) CHECK(c.start(1) == need);
+}
+
+static void line(const std::vector<PagedSeg>& segs, int hkv, int BM, int BLK, int grid) {
+  int64_t per_head = 0;
+  std::vector<int64_t> pre;
+  for (const PagedSeg& s : segs) {
+    pre.push_back(per_head);
+    if (s.lq > 0) per_head += paged_cost(s, BM, BLK).start(paged_row_blocks(s, BM));
+  }
+  const PagedRanges R = paged_ranges(per_head * hkv, grid);
+  CHECK(R.active <= grid && R.active * R.per >= R.all && (R.active == 0 || (R.active - 1) * R.per < R.all));
+  std::vector<int> taken(grid, 0);
+  for (int32_t b = 0; b < grid; ++b) {
+    const int32_t w = paged_range_of(b, R.active);
+    CHECK(w >= -1 && w < R.active);
+    if (w >= 0) CHECK(++taken[w] == 1);
+  }
+  for (int32_t w = 0; w < R.active; ++w) CHECK(taken[w] == 1);
+  for (int h = 0; h < hkv; ++h)
+    for (size_t b = 0; b < segs.size(); ++b) {
+      if (segs[b].lq == 0) continue;
+      const PagedCost c = paged_cost(segs[b], BM, BLK);
+      for (int32_t i = 0; i < c.n; ++i) {
+        const int64_t xs = h * per_head + pre[b] + c.start(i), v = paged_blocks(segs[b], BM, BLK, i);
+        const int64_t first = xs / R.per, last = (xs + v - 1) / R.per;
+        int64_t seen = 0;
+        for (int64_t w = first; w <= last; ++w) {
+          const int64_t lo = std::max(w * R.per, xs), hi = std::min((w + 1) * R.per, xs + v);
+          CHECK(lo < hi && w < R.active);
+          if (w > first) CHECK(lo == w * R.per);  // the one piece of its range that goes on from another
+          seen += hi - lo;
+        }
+        CHECK(seen == v);
+      }
+    }
+}
+
+int main() {
+  std::mt19937 rng(1);
+  auto pick = [&](int64_t lo, int64_t hi) {
+    const double x = std::uniform_real_distribution<double>(std::log((double)lo), std::log((double)hi + 1))(rng);
+    return (int32_t)std::min<int64_t>(hi, (int64_t)std::exp(x));
+  };
+  const int tiles[][2] = {{128, 64}, {32, 128}, {32, 256}, {32, 64}};
+  for (int n = 0; n < 30000; ++n) {
+    const int32_t group = n % 3 == 0 ? 1 << (rng() % 8) : pick(1, n % 5 == 0 ? 4096 : 16);
+    PagedSeg s{pick(1, n % 7 == 0 ? 40000 : 700), pick(1, n % 11 == 0 ? 2000000 : 9000) - 1, group, (int32_t)(rng() % 4 != 0)};
+    if ((int64_t)s.lq * group > 400000) s.lq = 400000 / group;
+    if (s.lq < 1) s.lq = 1;
+    const int* t = tiles[n % 4];
+    segment(s, t[0], t[1]);
+  }
+  for (int64_t lk : {0, 1, 63, 64, 65, 128, 1 << 20, (1 << 30) - 1})
+    for (int64_t lq : {1, 2, 127, 128, 129, 4096})
+      for (int group : {1, 3, 8, 128, 4096})
+        for (int causal : {0, 1})
+          for (const int* t : tiles) segment(PagedSeg{(int32_t)lq, (int32_t)lk, group, causal}, t[0], t[1]);
+  for (int n = 0; n < 3000; ++n) {
+    std::vector<PagedSeg> segs(rng() % 20);
+    const int32_t group = pick(1, 16), causal = rng() % 4 != 0;
+    for (PagedSeg& s : segs) s = PagedSeg{(int32_t)(rng() % 5 ? pick(1, 300) : 0), pick(1, 3000) - 1, group, causal};
+    const int* t = tiles[n % 4];
+    line(segs, 1 + rng() % 9, t[0], t[1], n % 2 ? 512 : 8 * (1 + rng() % 64));
+  }
+  std::puts("ok");
+}
