@@ -29,14 +29,14 @@ namespace {
 // A row of keys that are not there (never written).
 __device__ __attribute__((aligned(256))) uint32_t g_zero_row[64];
 
-// What the first workgroup of a shared row block leaves for the merge.
+// What the first workgroup of a shared row block leaves for the merge: its pieces lie at `first` and
+// then at next + i * step, i = 1 .. pieces - 1.
 struct PagedShare {
   int32_t pieces;  // 0: none
-  int32_t range;   // of its first workgroup
+  int32_t first, next, step;
   int32_t hk, rows;
   int32_t row0;    // first row (of the group's rows of this segment)
   int32_t q_start;
-  int32_t pad[2];
 };
 
 struct PagedParams {
@@ -51,9 +51,10 @@ struct PagedParams {
   const int32_t* kv_lens;
   const int32_t* cu_q;
   WsHeader* hdr;
-  PagedShare* share;  // [grid]
-  float2* stat;       // [grid][2][BM] (max in log2 units, sum)
-  float* part;        // [grid][2][BM][D]
+  PagedShare* share;  // [ranges], or [row blocks]
+  float2* stat;       // [pieces][BM] (max in log2 units, sum)
+  float* part;        // [pieces][BM][D]
+  int32_t parts;      // kItems: workgroups of a row block at most
   int64_t total_q;
   int32_t num_seqs, max_pages, page_shift, max_len;
   int32_t hq, hkv, group;
@@ -62,6 +63,7 @@ struct PagedParams {
 };
 
 constexpr int kTileBM = 128, kTileBN = 64, kPagedGrid = 512;
+constexpr int kPartTiles = 4;  // key tiles of a part at least
 
 struct PagedLds {
   int64_t pre[257];  // slots before the segments of each thread, per KV head
@@ -75,13 +77,27 @@ __device__ __forceinline__ PagedSeg paged_seg(const PagedParams& p, int32_t b) {
   return PagedSeg{p.cu_q[b + 1] - p.cu_q[b], p.kv_lens[b], p.group, p.causal};
 }
 
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
 __device__ __forceinline__ int64_t shfl_up64(int64_t x, int off) {
   const uint32_t lo = __shfl_up((uint32_t)x, off), hi = __shfl_up((uint32_t)((uint64_t)x >> 32), off);
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
 // Lays out the line (256 threads): pre[], and the slots per KV head; negative when the lengths are
-// refused.  Block 0 writes the header.
+// refused.  Block 0 writes the header.  BLK == 0: row blocks are counted instead.
+template <int BM, int BLK>
+__device__ __forceinline__ int64_t segment_cost(const PagedSeg& s) {
+  if constexpr (BLK == 0) {
+    return paged_row_blocks(s, BM);
+  } else {
+    const PagedCost c = paged_cost(s, BM, BLK);
+    return c.start(c.n);
+  }
+}
 template <int BM, int BLK>
 __device__ __forceinline__ int64_t paged_line(const PagedParams& p, PagedLds& L) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -98,10 +114,7 @@ __device__ __forceinline__ int64_t paged_line(const PagedParams& p, PagedLds& L)
     if (n < 0 || len < 0) code = BS_DEV_NOT_MONOTONE;
     else if (len > p.max_len) code = code == BS_DEV_OK ? BS_DEV_TOO_LONG : code;
     else if (n > p.total_q) code = BS_DEV_BAD_TOTAL;
-    else if (n > 0) {
-      const PagedCost c = paged_cost(PagedSeg{(int32_t)n, len, p.group, p.causal}, BM, BLK);
-      sum += c.start(c.n);
-    }
+    else if (n > 0) sum += segment_cost<BM, BLK>(PagedSeg{(int32_t)n, len, p.group, p.causal});
   }
   if (code != BS_DEV_OK) atomicCAS(&L.bad, BS_DEV_OK, code);
   int64_t run = sum;
@@ -124,45 +137,28 @@ __device__ __forceinline__ int64_t paged_line(const PagedParams& p, PagedLds& L)
   const int32_t bad = L.bad;
   if (blockIdx.x == 0 && tid == 0) {
     p.hdr->status = bad;
-    p.hdr->n_items = 0;
+    p.hdr->n_items = BLK == 0 && bad == BS_DEV_OK ? (int32_t)L.pre[256] : 0;  // row blocks per KV head
   }
-  return bad == BS_DEV_OK ? L.pre[256] : -1;
+  return uniform64(bad == BS_DEV_OK ? L.pre[256] : -1);
 }
 
-// The piece that starts at slot x.  All of it is the same in every lane.
-struct Piece {
-  int32_t hk, seg, q_start, lq, lk;
-  int32_t rb;      // row block
-  int32_t kb, n;   // key blocks [kb, kb + n) of the row block's v; n <= 0: slots behind them
-  int32_t v;
-  int64_t xs;      // the row block's first slot
-  int64_t next;    // the next row block's
-};
-
+// The segment that holds place y of the line, and the places before it.  The same in every lane.
 template <int BM, int BLK>
-__device__ __forceinline__ Piece paged_piece(const PagedParams& p, const PagedLds& L, int64_t line,
-                                             int64_t x, int64_t x_end) {
+__device__ __forceinline__ int32_t find_segment(const PagedParams& p, const PagedLds& L, int64_t y,
+                                                int64_t& before) {
   const int lane = threadIdx.x & 63;
-  Piece c;
-  int32_t hk = (int32_t)((double)x / (double)line);
-  if (hk * line > x) --hk;
-  if ((hk + 1) * line <= x) ++hk;
-  const int64_t y = x - hk * line;
   int t = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) t += __popcll(__ballot(L.pre[i * 64 + lane] <= y));
   const int32_t pt = seqs_per_thread(p.num_seqs);
-  int64_t before = L.pre[t];
+  before = L.pre[t];
   int32_t b = t;
   if (pt > 1) {  // (at most 64 segments per thread)
     const int32_t mine = t * pt + lane;
     int64_t cost = 0;
     if (lane < pt && mine < p.num_seqs) {
       const PagedSeg s = paged_seg(p, mine);
-      if (s.lq > 0) {
-        const PagedCost k = paged_cost(s, BM, BLK);
-        cost = k.start(k.n);
-      }
+      if (s.lq > 0) cost = segment_cost<BM, BLK>(s);
     }
     int64_t run = cost;
 #pragma unroll
@@ -176,24 +172,91 @@ __device__ __forceinline__ Piece paged_piece(const PagedParams& p, const PagedLd
     const uint32_t lo = __shfl((uint32_t)at, k), hi = __shfl((uint32_t)((uint64_t)at >> 32), k);
     before = (int64_t)(((uint64_t)hi << 32) | lo);
   }
-  b = __builtin_amdgcn_readfirstlane(b);
+  return __builtin_amdgcn_readfirstlane(b);
+}
+
+// A part of a row block.  All of it is the same in every lane.
+struct Piece {
+  int32_t hk, seg, q_start, lq, lk;
+  int32_t rb;      // row block
+  int32_t kb, n;   // key blocks [kb, kb + n) of the row block's v; n <= 0: slots behind them
+  int32_t v;
+  int32_t at;      // its place among the pieces, where the row block is shared
+  int64_t xs;      // kLine: the row block's first slot
+  int64_t next;    // and the next row block's
+};
+
+// The piece that starts at slot x.
+template <int BM, int BLK>
+__device__ __forceinline__ Piece paged_piece(const PagedParams& p, const PagedLds& L, int64_t line,
+                                             int64_t x, int64_t x_end, int32_t range) {
+  Piece c;
+  int32_t hk = (int32_t)((double)x / (double)line);
+  if (hk * line > x) --hk;
+  if ((hk + 1) * line <= x) ++hk;
+  const int64_t y = x - hk * line;
+  int64_t before;
+  c.seg = find_segment<BM, BLK>(p, L, y, before);
   c.hk = __builtin_amdgcn_readfirstlane(hk);
-  c.seg = b;
-  c.q_start = p.cu_q[b];
-  const PagedSeg s = paged_seg(p, b);
-  c.lq = s.lq;
-  c.lk = s.lk;
+  const PagedSeg s = paged_seg(p, c.seg);
+  c.q_start = __builtin_amdgcn_readfirstlane(p.cu_q[c.seg]);
+  c.lq = __builtin_amdgcn_readfirstlane(s.lq);
+  c.lk = __builtin_amdgcn_readfirstlane(s.lk);
   const PagedCost k = paged_cost(s, BM, BLK);
   c.rb = __builtin_amdgcn_readfirstlane(k.find(y - before));
   const int64_t first = before + k.start(c.rb);
-  c.xs = hk * line + first;
-  c.next = hk * line + before + k.start(c.rb + 1);
+  c.xs = uniform64(hk * line + first);
+  c.next = uniform64(hk * line + before + k.start(c.rb + 1));
   c.kb = __builtin_amdgcn_readfirstlane((int32_t)(y - first));
   c.v = __builtin_amdgcn_readfirstlane(paged_blocks(s, BM, BLK, c.rb));
   const int64_t left = x_end - x;
   const int32_t rest = c.v - c.kb;
   c.n = __builtin_amdgcn_readfirstlane(rest < left ? rest : (int32_t)left);
+  // a range has at most one piece that goes on from the range before (place 0 of its two) and one that
+  // another range goes on with (place 1)
+  c.at = range * 2 + (c.kb == 0);
   return c;
+}
+
+// The piece of workgroup b: a part of a row block, the row blocks of one segment and head side by side on one
+// XCD (b % 8), the longest first; line: row blocks per KV head.  false: none.
+template <int BM, int BLK>
+__device__ __forceinline__ bool paged_item(const PagedParams& p, const PagedLds& L, int64_t line, int32_t b,
+                                           Piece& c) {
+  const bool own = (p.hkv & 7) == 0;  // each XCD owns an eighth of the heads
+  const int32_t hx = own ? p.hkv >> 3 : p.hkv, j = own ? b >> 3 : b;
+  const int32_t i = j / (hx * p.parts);  // a row block's place, if all heads took turns
+  if (i >= line) return false;
+  int64_t before;
+  c.seg = find_segment<BM, 0>(p, L, i, before);
+  const PagedSeg s = paged_seg(p, c.seg);
+  c.q_start = __builtin_amdgcn_readfirstlane(p.cu_q[c.seg]);
+  c.lq = __builtin_amdgcn_readfirstlane(s.lq);
+  c.lk = __builtin_amdgcn_readfirstlane(s.lk);
+  const int32_t nrb = paged_row_blocks(s, BM);
+  const int32_t r = j - (int32_t)before * hx * p.parts;  // of the segment's nrb * hx * parts
+  int32_t hl, u;  // head; row block and part
+  if (own) {
+    hl = r / (nrb * p.parts);
+    u = r - hl * nrb * p.parts;
+  } else {
+    u = r / hx;
+    hl = r - u * hx;
+  }
+  const int32_t back = u / p.parts, part = u - back * p.parts;
+  c.hk = __builtin_amdgcn_readfirstlane(own ? (b & 7) * hx + hl : hl);
+  c.rb = __builtin_amdgcn_readfirstlane(nrb - 1 - back);
+  c.v = __builtin_amdgcn_readfirstlane(paged_blocks(s, BM, BLK, c.rb));
+  const int32_t parts = min(p.parts, max(1, c.v / kPartTiles));
+  if (part >= parts) {
+    c.n = 0;
+    return true;
+  }
+  c.kb = part * c.v / parts;
+  c.n = (part + 1) * c.v / parts - c.kb;
+  // pieces and shares are numbered by head and row block
+  c.at = __builtin_amdgcn_readfirstlane((c.hk * (int32_t)line + (int32_t)before + c.rb) * p.parts + part);
+  return true;
 }
 
 // One wave's copy of 16 rows (row r from src + min(r, last) * stride bytes) into 16 rows of a swizzled
@@ -208,7 +271,8 @@ __device__ __forceinline__ void copy16(bf16* lds, const char* src, int stride, i
 
 constexpr float kRescaleBy = 8.0f;  // log2 units (fwd_bf16.hip)
 
-template <int D>
+// kLine: a workgroup per range of the line; otherwise per part of a row block.
+template <int D, bool kLine>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_tile_kernel(const PagedParams p) {
   constexpr int BM = kTileBM, BN = kTileBN, TILE = BN * D, KK = D / 16, DB = D / 32;
@@ -221,46 +285,60 @@ void paged_tile_kernel(const PagedParams p) {
 
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hh = lane >> 5;
-  const int64_t line = paged_line<BM, BN>(p, L);
-  PagedShare* share = p.share + blockIdx.x;
+  const int64_t line = paged_line<BM, kLine ? BN : 0>(p, L);
   if (line < 0) return;
-  const PagedRanges R = paged_ranges(line * p.hkv, gridDim.x);
-  const int32_t range = paged_range_of(blockIdx.x, R.active);
-  if (range < 0) {
-    if (tid == 0) share->pieces = 0;
-    return;
+  PagedShare* share = nullptr;
+  PagedRanges R;
+  int32_t range = 0;
+  int64_t x = 0, x_end = 1;
+  if constexpr (kLine) {
+    share = p.share + blockIdx.x;
+    R = paged_ranges(line * p.hkv, gridDim.x);
+    R.per = uniform64(R.per);
+    R.active = __builtin_amdgcn_readfirstlane(R.active);
+    range = paged_range_of(blockIdx.x, R.active);
+    if (range < 0) {
+      if (tid == 0) share->pieces = 0;
+      return;
+    }
+    x = range * R.per;
+    x_end = min(R.all, x + R.per);
   }
-  int64_t x = range * R.per;
-  const int64_t x_end = min(R.all, x + R.per);
   bool left_share = false;
   const int group = p.group;
   const float c2 = p.scale_log2;
   const int tstride = (int)p.token_stride;
+  const int rbase = swz_row_base<D>(lane), tbase = swz_tr_base<D>(lane);
 
   while (x < x_end) {
-    const Piece e = paged_piece<BM, BN>(p, L, line, x, x_end);
-    if (e.n <= 0) {
-      x = e.next;
-      continue;
+    Piece e;
+    if constexpr (kLine) {
+      e = paged_piece<BM, BN>(p, L, line, x, x_end, range);
+      if (e.n <= 0) {
+        x = e.next;
+        continue;
+      }
+      x = e.kb + e.n == e.v ? e.next : x_end;
+    } else {
+      if (!paged_item<BM, BN>(p, L, line, blockIdx.x, e) || e.n == 0) return;
+      x = x_end;
     }
-    x = e.kb + e.n == e.v ? e.next : x_end;
     const int rows = min((int)(e.lq * group - e.rb * BM), BM);
     const int qrow = w * 32 + c;
     const bool qvalid = qrow < rows;
     const uint32_t r_lane = (uint32_t)(e.rb * BM + (qvalid ? qrow : 0));
-    const int qi = (int)(r_lane / (uint32_t)group), head = e.hk * group + (int)r_lane - qi * group;
-    const int64_t orow = ((int64_t)e.q_start + qi) * p.hq + head;
     bf16x8 qf[KK];
+    int lim_base;  // keys below it are visible to this lane's query (less the lane half's offset)
     {
+      const int qi = (int)(r_lane / (uint32_t)group), head = e.hk * group + (int)r_lane - qi * group;
+      const int64_t orow = ((int64_t)e.q_start + qi) * p.hq + head;
+      lim_base = (p.causal ? min(e.lk, qi + e.lk - e.lq + 1) : e.lk) - hh * 4;
       const bf16* qp = static_cast<const bf16*>(p.q) + orow * D + hh * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 16);
     }
-    const int diag = e.lk - e.lq;
-    // keys below lim_base are visible to this lane's query (less the lane half's offset)
-    const int lim_base = (p.causal ? min(e.lk, qi + diag + 1) : e.lk) - hh * 4;
     int full = e.lk;
-    if (p.causal) full = min(full, (int)((uint32_t)(e.rb * BM) / (uint32_t)group) + diag + 1);
+    if (p.causal) full = min(full, (int)((uint32_t)(e.rb * BM) / (uint32_t)group) + e.lk - e.lq + 1);
     const int n_full = full > 0 ? full / BN : 0;
     const int t0 = e.kb, n_tiles = e.kb + e.n;
     const int keys = e.lk;
@@ -306,9 +384,17 @@ void paged_tile_kernel(const PagedParams p) {
       for (int kk = 0; kk < KK; ++kk) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          const bf16x8 a = *reinterpret_cast<const bf16x8*>(&Kb[swz_off<D>(kb * 32 + c, kk * 2 + hh)]);
+          const bf16x8 a = lds_row16(Kb, (rbase ^ (kk << 5)) + kb * 64 * D);
           sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], sacc[kb], 0, 0, 0);
         }
+      }
+      // K reads two contraction steps ahead of the products, copies spread among them (fwd_bf16.hip)
+      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
+        if constexpr (more()) __builtin_amdgcn_sched_group_barrier(kSchedVmem, 1, 0);
+        if (kk + 2 < KK) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
       }
       if (t >= n_full) {
         const int lim = lim_base - t * BN;
@@ -353,8 +439,8 @@ void paged_tile_kernel(const PagedParams p) {
       for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const bf16x8 a = lds_read_tr2(Vb + swz_tr_off<D>(ks * 16, db * 32, 0, lane),
-                                        Vb + swz_tr_off<D>(ks * 16, db * 32, 1, lane));
+          const bf16x8 a = lds_tr16(Vb, (tbase ^ (db << 6)) + ks * 32 * D,
+                                    (tbase ^ ((db << 6) | 32)) + ks * 32 * D + 16 * D);
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[ks], oacc[db], 0, 0, 0);
         }
       }
@@ -376,21 +462,23 @@ void paged_tile_kernel(const PagedParams p) {
 
     const float l_tot = half_sum(l_run);
     const bool whole = e.n == e.v;
-    // a range has at most one piece that goes on from the range before (slot 0) and one that another
-    // range goes on with (slot 1)
-    const int slot = e.kb == 0;
-    if (!whole && slot) {
-      left_share = true;
-      if (tid == 0) {
-        share->pieces = (int32_t)((e.xs + e.v - 1) / R.per - e.xs / R.per) + 1;
-        share->range = range;
-        share->hk = e.hk;
-        share->rows = rows;
-        share->row0 = e.rb * BM;
-        share->q_start = e.q_start;
+    if constexpr (kLine) {
+      if (!whole && e.kb == 0) {
+        left_share = true;
+        if (tid == 0)
+          *share = PagedShare{(int32_t)((e.xs + e.v - 1) / R.per - e.xs / R.per) + 1, e.at, range * 2, 2, e.hk, rows,
+                              e.rb * BM, e.q_start};
       }
+    } else if (p.parts > 1 && e.kb == 0) {
+      const int32_t parts = whole ? 0 : min(p.parts, e.v / kPartTiles);
+      if (tid == 0)
+        p.share[e.at / p.parts] = PagedShare{parts, e.at, e.at, 1, e.hk, rows, e.rb * BM, e.q_start};
     }
     if (qvalid && whole) {
+      uint32_t r = r_lane;
+      asm volatile("" : "+v"(r));  // the row's place is worked out again: held over the loop, registers spill
+      const int qi = (int)(r / (uint32_t)group), head = e.hk * group + (int)r - qi * group;
+      const int64_t orow = ((int64_t)e.q_start + qi) * p.hq + head;
       const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
       bf16* op = static_cast<bf16*>(p.o) + orow * D + hh * 4;
 #pragma unroll
@@ -403,7 +491,7 @@ void paged_tile_kernel(const PagedParams p) {
       if (hh == 0)
         p.lse[head * p.total_q + e.q_start + qi] = l_tot > 0.f ? (m2 + log2f(l_tot)) * kLn2 : -INFINITY;
     } else if (qvalid) {
-      const int64_t at = ((int64_t)range * 2 + slot) * BM + qrow;
+      const int64_t at = (int64_t)e.at * BM + qrow;
       float* op = p.part + at * D + hh * 4;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
@@ -414,20 +502,22 @@ void paged_tile_kernel(const PagedParams p) {
       if (hh == 0) p.stat[at] = make_float2(m2, l_tot);
     }
   }
-  if (!left_share && tid == 0) share->pieces = 0;
+  if constexpr (kLine)
+    if (!left_share && tid == 0) share->pieces = 0;
 }
 
 // Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, D/4 lanes per
-// row.  The pieces are those of consecutive ranges: the first's slot 1, then slots 0.
-template <int D, int BM>
+// row.  kLine: by ranges, otherwise by row blocks.
+template <int D, int BM, bool kLine>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
   constexpr int LPR = D / 4;
   if (p.hdr->status != BS_DEV_OK) return;
+  if (!kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;
   const PagedShare s = p.share[blockIdx.x];
   if (s.pieces == 0) return;
   const int row = blockIdx.y * (256 / LPR) + threadIdx.x / LPR, ch = threadIdx.x % LPR;
   if (row >= s.rows) return;
-  auto at = [&](int i) { return (((int64_t)s.range + i) * 2 + (i == 0)) * BM + row; };
+  auto at = [&](int i) { return (int64_t)(i == 0 ? s.first : s.next + i * s.step) * BM + row; };
   float M = -INFINITY;
   for (int i = 0; i < s.pieces; ++i) M = fmaxf(M, p.stat[at(i)].x);
   const float base = M == -INFINITY ? 0.f : M;
@@ -510,34 +600,49 @@ __global__ __launch_bounds__(256) void paged_row_kernel(const PagedParams p) {
   if (lane == 0) p.lse[h * p.total_q + tok] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Workspace: header, shares, statistics and sums of the ranges' pieces.
+// What a call launches, from its shapes alone, and its workspace: header, shares, statistics and sums
+// of the pieces.
 struct PagedLayout {
-  int32_t grid;
+  bool line;
+  int32_t grid;    // workgroups
+  int32_t parts;   // !line: of a row block
+  int32_t shares;  // shares, and so workgroups in x of the merge (0: no merge)
   size_t share, stat, part, bytes;
 };
-PagedLayout paged_layout(const bs_dims& d) {
+PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs) {
   PagedLayout L = {};
-  if (d.dtype == BS_F32) {
-    L.bytes = sizeof(WsHeader);
-    return L;
+  L.share = L.stat = L.part = L.bytes = sizeof(WsHeader);
+  if (d.dtype == BS_F32) return L;
+  const int64_t rows = d.total_q * (d.hq / d.hkv);
+  const int64_t blocks = num_seqs == 0 ? 0 : rows / kTileBM + (rows < num_seqs ? rows : num_seqs);  // per KV head at most
+  int64_t pieces;
+  L.line = num_seqs == 0 || rows <= 2 * kTileBM * (int64_t)num_seqs;
+  if (L.line) {
+    L.grid = L.shares = kPagedGrid;
+    pieces = 2 * kPagedGrid;
+  } else {
+    const int64_t items = blocks * d.hkv;
+    L.parts = items >= kPagedGrid ? 1 : (int32_t)(2 * kPagedGrid / items < 8 ? 2 * kPagedGrid / items : 8);
+    L.grid = (int32_t)(items * L.parts);
+    L.shares = L.parts > 1 ? (int32_t)items : 0;
+    pieces = L.parts > 1 ? items * L.parts : 0;
   }
-  L.grid = kPagedGrid;
-  L.share = sizeof(WsHeader);
-  L.stat = L.share + align256(sizeof(PagedShare) * (size_t)L.grid);
-  L.part = L.stat + align256(sizeof(float2) * 2 * kTileBM * (size_t)L.grid);
-  L.bytes = L.part + sizeof(float) * 2 * kTileBM * (size_t)L.grid * d.head_dim;
+  if (L.shares == 0) return L;
+  L.stat = L.share + align256(sizeof(PagedShare) * (size_t)L.shares);
+  L.part = L.stat + align256(sizeof(float2) * kTileBM * (size_t)pieces);
+  L.bytes = L.part + sizeof(float) * kTileBM * (size_t)pieces * d.head_dim;
   return L;
 }
 
 }  // namespace
 
-size_t paged_bytes(const bs_dims& d, int32_t, int32_t) { return paged_layout(d).bytes; }
+size_t paged_bytes(const bs_dims& d, int32_t num_seqs, int32_t) { return paged_layout(d, num_seqs).bytes; }
 
 hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cache& C,
                             const int32_t* cu_q, int32_t num_seqs, int32_t max_seqlen_k, int causal,
                             float scale, void* out, float* lse, void* ws, hipStream_t stream) {
   const int es = d.dtype == BS_BF16 ? 2 : 4;
-  const PagedLayout W = paged_layout(d);
+  const PagedLayout W = paged_layout(d, num_seqs);
   char* base = static_cast<char*>(ws);
   PagedParams p;
   p.q = q;
@@ -557,6 +662,7 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   p.share = reinterpret_cast<PagedShare*>(base + W.share);
   p.stat = reinterpret_cast<float2*>(base + W.stat);
   p.part = reinterpret_cast<float*>(base + W.part);
+  p.parts = W.parts;
   p.total_q = d.total_q;
   p.num_seqs = num_seqs;
   p.max_pages = C.max_pages;
@@ -569,14 +675,20 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   p.causal = causal;
   p.scale_log2 = scale * kLog2e;
   if (d.dtype == BS_BF16) {
-    const dim3 grid((unsigned)W.grid), mgrid((unsigned)W.grid, (unsigned)(kTileBM * d.head_dim / 1024));
-#define BS_CALL(D)                                                                            \
-  do {                                                                                        \
-    hipLaunchKernelGGL((paged_tile_kernel<D>), grid, dim3(256), 0, stream, p);                \
-    hipLaunchKernelGGL((paged_merge_kernel<D, kTileBM>), mgrid, dim3(256), 0, stream, p);     \
+    const dim3 grid((unsigned)W.grid), mgrid((unsigned)W.shares, (unsigned)(kTileBM * d.head_dim / 1024));
+#define BS_LAUNCH(D, LINE)                                                                         \
+  do {                                                                                             \
+    hipLaunchKernelGGL((paged_tile_kernel<D, LINE>), grid, dim3(256), 0, stream, p);               \
+    if (W.shares > 0)                                                                              \
+      hipLaunchKernelGGL((paged_merge_kernel<D, kTileBM, LINE>), mgrid, dim3(256), 0, stream, p);  \
+  } while (0)
+#define BS_CALL(D)                                             \
+  do {                                                         \
+    if (W.line) BS_LAUNCH(D, true); else BS_LAUNCH(D, false);  \
   } while (0)
     if (d.head_dim == 128) BS_CALL(128); else BS_CALL(64);
 #undef BS_CALL
+#undef BS_LAUNCH
     return hipGetLastError();
   }
   const dim3 grid((unsigned)((d.total_q * d.hq + 3) / 4 + (d.total_q == 0)));
