@@ -62,7 +62,7 @@ struct PagedParams {
   float scale_log2;
 };
 
-constexpr int kTileBM = 128, kTileBN = 64, kPagedGrid = 512;
+constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32, kPagedGrid = 512;
 constexpr int kPartTiles = 4;  // key tiles of a part at least
 
 struct PagedLds {
@@ -261,12 +261,12 @@ __device__ __forceinline__ bool paged_item(const PagedParams& p, const PagedLds&
 
 // One wave's copy of 16 rows (row r from src + min(r, last) * stride bytes) into 16 rows of a swizzled
 // tile, as dma_tile copies them.
-template <int D>
+template <int D, int AUX = 0>
 __device__ __forceinline__ void copy16(bf16* lds, const char* src, int stride, int last, int lane) {
   constexpr int CPR = D / 8, PER = 16 / (64 / CPR);
   const __amdgpu_buffer_rsrc_t rs =
       __builtin_amdgcn_make_buffer_rsrc((void*)(src - 4096), 0, 0x7fffffff, 0x00020000);
-  DmaRun<0, PER, D, 0>::issue(rs, lds, 0, lane / CPR, lane % CPR, stride >> 1, last);
+  DmaRun<0, PER, D, AUX>::issue(rs, lds, 0, lane / CPR, lane % CPR, stride >> 1, last);
 }
 
 constexpr float kRescaleBy = 8.0f;  // log2 units (fwd_bf16.hip)
@@ -506,6 +506,267 @@ void paged_tile_kernel(const PagedParams p) {
     if (!left_share && tid == 0) share->pieces = 0;
 }
 
+// Waits until at most N of this wave's copies are under way; until its LDS reads have returned (few_bf16.hip).
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | N);  // vmcnt(N), N < 16
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Few rows: 32 of them, and the four waves take the key tiles of a block of 4 KT keys, each with LDS buffers,
+// page numbers and a softmax of its own; the layout is that of few_bf16.hip.  Per tile a wave reads the
+// numbers of its KT / 16 pages in one load, a tile ahead of the copies that need them.
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void paged_few_kernel(const PagedParams p) {
+  constexpr int BM = kFewBM, KT = D == 128 ? 32 : 64, BLK = 4 * KT, NC = KT / 16;
+  constexpr int KB = KT / 32, KK = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) bf16 Kt[4][KT * D];
+  __shared__ __attribute__((aligned(16))) bf16 Vt[4][KT * D];
+  __shared__ PagedLds L;
+  __shared__ float Ms[4][32], Ls[4][32];
+
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hh = lane >> 5;
+  const int64_t line = paged_line<BM, BLK>(p, L);
+  if (line < 0) return;
+  PagedShare* share = p.share + blockIdx.x;
+  PagedRanges R = paged_ranges(line * p.hkv, gridDim.x);
+  R.per = uniform64(R.per);
+  R.active = __builtin_amdgcn_readfirstlane(R.active);
+  const int32_t range = paged_range_of(blockIdx.x, R.active);
+  if (range < 0) {
+    if (tid == 0) share->pieces = 0;
+    return;
+  }
+  int64_t x = range * R.per;
+  const int64_t x_end = min(R.all, x + R.per);
+  bool left_share = false;
+  const int group = p.group;
+  const float c2 = p.scale_log2;
+  const int tstride = (int)p.token_stride;
+  const int rbase = swz_row_base<D>(lane), tbase = swz_tr_base<D>(lane);
+  bf16* Kw = Kt[w];
+  bf16* Vw = Vt[w];
+
+  while (x < x_end) {
+    const Piece e = paged_piece<BM, BLK>(p, L, line, x, x_end, range);
+    if (e.n <= 0) {
+      x = e.next;
+      continue;
+    }
+    x = e.kb + e.n == e.v ? e.next : x_end;
+    const int rows = min((int)(e.lq * group - e.rb * BM), BM);
+    const uint32_t r_lane = (uint32_t)(e.rb * BM + min(c, rows - 1));
+    const int qi = (int)(r_lane / (uint32_t)group), hg = (int)r_lane - qi * group;
+    bf16x8 qf[KK];
+    {
+      const bf16* qp = static_cast<const bf16*>(p.q) +
+                       (((int64_t)e.q_start + qi) * p.hq + e.hk * group + hg) * D + hh * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 16);
+    }
+    const int keys = e.lk;
+    const int lim_lane = (p.causal ? min(keys, qi + keys - e.lq + 1) : keys) - hh * 4;
+    // keys some row sees, and this piece's end
+    int k_end = keys;
+    if (p.causal) k_end = min(k_end, (int)((uint32_t)(e.rb * BM + rows - 1) / (uint32_t)group) + keys - e.lq + 1);
+    if (e.kb + e.n < e.v) k_end = min(k_end, (e.kb + e.n) * BLK);
+
+    const int32_t* table = p.table + e.seg * p.table_stride;
+    const int64_t hoff = e.hk * p.head_stride;
+    // lane i < NC: page of keys k .. k + 15 of its part of the tile at k0 (-1: behind the sequence's end)
+    auto pages_of = [&](int k0) {
+      const int key = k0 + lane * 16;
+      return lane < NC && key < keys ? table[key >> p.page_shift] : -1;
+    };
+    // what a tile's copies need: place and stride of each 16 keys, their last row; the missing ones
+    struct Place {
+      int64_t off[NC];
+      int there, miss;
+    };
+    auto place_of = [&](int pages, int k0) {
+      Place a;
+      a.there = a.miss = 0;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int page = __builtin_amdgcn_readlane(pages, i), key = k0 + i * 16;
+        const bool there = page >= 0 && page < p.num_pages;
+        a.off[i] = page * p.page_stride + (int64_t)(key & ((1 << p.page_shift) - 1)) * tstride + hoff;
+        a.there |= there << i;
+        a.miss |= (!there && key < keys) << i;
+      }
+      return a;
+    };
+    auto copy = [&](bf16* dst, const char* cache, const Place& a, int k0) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const bool there = (a.there >> i) & 1;
+        const char* src = there ? cache + a.off[i] : reinterpret_cast<const char*>(g_zero_row);
+        const int last = min(15, keys - 1 - k0 - i * 16);
+        copy16<D, 2>(dst + i * 16 * D, src, there ? tstride : 0, last < 0 ? 0 : last, lane);
+      }
+    };
+
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+    float m2 = -INFINITY, l_run = 0.f;
+
+    int k0 = (e.kb * 4 + w) * KT;
+    Place now;
+    int ahead = -1;  // pages of the next tile
+    // one tile; `more`: another follows (straight-line forms, so that the copies under way can be counted)
+    auto step = [&](auto more) {
+      wait_copies<8>();  // K has landed (V's eight copies may be under way)
+      f32x16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const bf16x8 a = lds_row16(Kw, (rbase ^ (kk << 5)) + kb * 64 * D);
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], s[kb], 0, 0, 0);
+        }
+      const int next = k0 + BLK, miss = now.miss;
+      wait_reads();
+      if constexpr (more()) {
+        now = place_of(ahead, next);
+        ahead = pages_of(next + BLK);
+        copy(Kw, p.kc, now, next);
+      }
+      const int lim = lim_lane - k0;
+      if (k0 + KT > keys || p.causal) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[kb][r] = (kb * 32 + (r >> 2) * 8 + (r & 3)) < lim ? s[kb][r] : -INFINITY;
+      }
+      if (miss) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[kb][r] = (miss >> (kb * 2 + (r >> 3))) & 1 ? -INFINITY : s[kb][r];
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+      mx = half_max(mx) * c2;
+      if (__any(mx > m2)) {
+        const float m_new = fmaxf(m2, mx);
+        const float alpha = fast_exp2(m2 - (m_new == -INFINITY ? 0.f : m_new));
+        m2 = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      }
+      const float base = m2 == -INFINITY ? 0.f : m2;
+      bf16x8 pb[2 * KB];  // P rounded to bf16 for the product; the sum takes it in float32
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float ex = fast_exp2(fmaf(s[kb][r], c2, -base));
+          l_run += ex;
+          pb[kb * 2 + (r >> 3)][r & 7] = f2bf(ex);
+        }
+      // V has landed.  (At most K's eight copies and the pages' load come after it; where the load is
+      // moved, waiting for one operation more than needed is all that happens.)
+      wait_copies<more() ? 8 : 0>();
+#pragma unroll
+      for (int ks = 0; ks < 2 * KB; ++ks)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const bf16x8 a = lds_tr16(Vw, (tbase ^ (db << 6)) + ks * 32 * D,
+                                    (tbase ^ ((db << 6) | 32)) + ks * 32 * D + 16 * D);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[ks], oacc[db], 0, 0, 0);
+        }
+      wait_reads();
+      if constexpr (more()) copy(Vw, p.vc, now, next);
+      k0 = next;
+    };
+    if (k0 < k_end) {
+      now = place_of(pages_of(k0), k0);
+      ahead = pages_of(k0 + BLK);
+      copy(Kw, p.kc, now, k0);
+      copy(Vw, p.vc, now, k0);
+      // Q is waited for here: left to the loop, the compiler would wait for every copy there
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
+      while (k0 + BLK < k_end) step(std::true_type{});
+      step(std::false_type{});
+    }
+
+    // combine the four waves' (max, sum, O) through their own buffers (as few_bf16.hip)
+    const float l_tot = half_sum(l_run);
+    if (hh == 0) {
+      Ms[w][c] = m2;
+      Ls[w][c] = l_tot;
+    }
+    __syncthreads();
+    float M = -INFINITY, Lt = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, Ms[i][c]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float mi = Ms[i][c];
+      Lt += Ls[i][c] * (mi == -INFINITY ? 0.f : fast_exp2(mi - M));
+    }
+    const bool whole = e.n == e.v;
+    float wgt = m2 == -INFINITY ? 0.f : fast_exp2(m2 - M);
+    if (whole) wgt *= Lt > 0.f ? 1.f / Lt : 0.f;
+    auto area = [&](int wv, int ch) {  // chunk ch (head_dim 4 ch ..) of row 0
+      return reinterpret_cast<char*>(ch < 16 ? Kt[wv] : Vt[wv]);
+    };
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int ch = db * 8 + a * 2 + hh;
+        const f32x4 o4 = {oacc[db][a * 4] * wgt, oacc[db][a * 4 + 1] * wgt,
+                          oacc[db][a * 4 + 2] * wgt, oacc[db][a * 4 + 3] * wgt};
+        *reinterpret_cast<f32x4*>(area(w, db * 8) + c * 256 + (((ch & 15) ^ (c & 15)) << 4)) = o4;
+      }
+    if (!whole && e.kb == 0) {
+      left_share = true;
+      if (tid == 0)
+        *share = PagedShare{(int32_t)((e.xs + e.v - 1) / R.per - e.xs / R.per) + 1, e.at, range * 2, 2, e.hk, rows,
+                            e.rb * BM, e.q_start};
+    }
+    if (w == 0 && hh == 0 && c < rows) {
+      if (whole)
+        p.lse[(e.hk * group + hg) * p.total_q + e.q_start + qi] = Lt > 0.f ? (M + log2f(Lt)) * kLn2 : -INFINITY;
+      else p.stat[(int64_t)e.at * BM + c] = make_float2(M, Lt);
+    }
+    __syncthreads();
+    for (int u = tid; u < rows * (D / 4); u += 256) {
+      const int r = u / (D / 4), ch = u % (D / 4);
+      const int at = r * 256 + (((ch & 15) ^ (r & 15)) << 4);
+      f32x4 o4 = *reinterpret_cast<const f32x4*>(area(0, ch) + at);
+#pragma unroll
+      for (int i = 1; i < 4; ++i) o4 += *reinterpret_cast<const f32x4*>(area(i, ch) + at);
+      if (whole) {
+        const uint32_t rr = (uint32_t)(e.rb * BM + r);
+        const int ri = (int)(rr / (uint32_t)group);
+        const int64_t row = ((int64_t)e.q_start + ri) * p.hq + e.hk * group + (int)rr - ri * group;
+        *reinterpret_cast<bf16x4*>(static_cast<bf16*>(p.o) + row * D + ch * 4) =
+            bf16x4{f2bf(o4[0]), f2bf(o4[1]), f2bf(o4[2]), f2bf(o4[3])};
+      } else {
+        *reinterpret_cast<f32x4*>(p.part + ((int64_t)e.at * BM + r) * D + ch * 4) = o4;
+      }
+    }
+    __syncthreads();  // the buffers are free
+  }
+  if (!left_share && tid == 0) share->pieces = 0;
+}
+
 // Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, D/4 lanes per
 // row.  kLine: by ranges, otherwise by row blocks.
 template <int D, int BM, bool kLine>
@@ -603,7 +864,8 @@ __global__ __launch_bounds__(256) void paged_row_kernel(const PagedParams p) {
 // What a call launches, from its shapes alone, and its workspace: header, shares, statistics and sums
 // of the pieces.
 struct PagedLayout {
-  bool line;
+  bool few, line;
+  int32_t bm;      // rows of a block
   int32_t grid;    // workgroups
   int32_t parts;   // !line: of a row block
   int32_t shares;  // shares, and so workgroups in x of the merge (0: no merge)
@@ -616,6 +878,8 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs) {
   const int64_t rows = d.total_q * (d.hq / d.hkv);
   const int64_t blocks = num_seqs == 0 ? 0 : rows / kTileBM + (rows < num_seqs ? rows : num_seqs);  // per KV head at most
   int64_t pieces;
+  L.few = rows <= kFewBM * (int64_t)num_seqs;
+  L.bm = L.few ? kFewBM : kTileBM;
   L.line = num_seqs == 0 || rows <= 2 * kTileBM * (int64_t)num_seqs;
   if (L.line) {
     L.grid = L.shares = kPagedGrid;
@@ -629,8 +893,8 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs) {
   }
   if (L.shares == 0) return L;
   L.stat = L.share + align256(sizeof(PagedShare) * (size_t)L.shares);
-  L.part = L.stat + align256(sizeof(float2) * kTileBM * (size_t)pieces);
-  L.bytes = L.part + sizeof(float) * kTileBM * (size_t)pieces * d.head_dim;
+  L.part = L.stat + align256(sizeof(float2) * L.bm * (size_t)pieces);
+  L.bytes = L.part + sizeof(float) * L.bm * (size_t)pieces * d.head_dim;
   return L;
 }
 
@@ -675,16 +939,23 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   p.causal = causal;
   p.scale_log2 = scale * kLog2e;
   if (d.dtype == BS_BF16) {
-    const dim3 grid((unsigned)W.grid), mgrid((unsigned)W.shares, (unsigned)(kTileBM * d.head_dim / 1024));
+    const dim3 grid((unsigned)W.grid), mgrid((unsigned)W.shares, (unsigned)(W.bm * d.head_dim / 1024));
 #define BS_LAUNCH(D, LINE)                                                                         \
   do {                                                                                             \
     hipLaunchKernelGGL((paged_tile_kernel<D, LINE>), grid, dim3(256), 0, stream, p);               \
     if (W.shares > 0)                                                                              \
       hipLaunchKernelGGL((paged_merge_kernel<D, kTileBM, LINE>), mgrid, dim3(256), 0, stream, p);  \
   } while (0)
-#define BS_CALL(D)                                             \
-  do {                                                         \
-    if (W.line) BS_LAUNCH(D, true); else BS_LAUNCH(D, false);  \
+#define BS_CALL(D)                                                                                  \
+  do {                                                                                              \
+    if (W.few) {                                                                                    \
+      hipLaunchKernelGGL((paged_few_kernel<D>), grid, dim3(256), 0, stream, p);                     \
+      hipLaunchKernelGGL((paged_merge_kernel<D, kFewBM, true>), mgrid, dim3(256), 0, stream, p);    \
+    } else if (W.line) {                                                                            \
+      BS_LAUNCH(D, true);                                                                           \
+    } else {                                                                                        \
+      BS_LAUNCH(D, false);                                                                          \
+    }                                                                                               \
   } while (0)
     if (d.head_dim == 128) BS_CALL(128); else BS_CALL(64);
 #undef BS_CALL
