@@ -276,6 +276,10 @@ int bs_attn_paged_fwd(const bs_dims* dims, const void* q, const bs_paged_cache* 
   if (overlaps(out, bytes, cache->k, cb) || overlaps(out, bytes, cache->v, cb))
     return fail(BS_ERR_INVALID_ARG, "out overlaps the cache");
   BS_TRY(check_scale(scale));
+  const int64_t room = (int64_t)cache->max_pages * cache->page_size, most = max_seqlen_k < room ? max_seqlen_k : room;
+  if (!paged_fits(d, num_seqs, max_seqlen_k, most))
+    return fail(BS_ERR_UNSUPPORTED, "%lld rows of %d sequences over up to %lld keys are too many for one call",
+                (long long)(d.total_q * d.hq), num_seqs, (long long)most);
   const size_t need = paged_bytes(d, num_seqs, max_seqlen_k);
   if (workspace == nullptr) return fail(BS_ERR_WORKSPACE, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)

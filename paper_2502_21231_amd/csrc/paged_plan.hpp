@@ -7,7 +7,7 @@
 //
 // With a causal mask v(i) grows with i, and its sum has no closed form because of the rounding.  The
 // line therefore gives row block i the slots [S(i), S(i + 1)) of
-//   S(i) = floor(i (A + i B)),  A + B (2 i + 1) >= v(i) + 1 / BLK,
+//   S(i) = floor(i (A + i B)),  A + B (2 i + 1) >= v(i) + 1 / BLK
 // a sum of the unrounded counts: S(i + 1) - S(i) >= floor(A + B (2 i + 1)) >= v(i), about one slot
 // more than needed on average.  The slots behind the v(i)-th are skipped.  The one row block of a
 // short segment has its v exactly.
@@ -49,9 +49,10 @@ struct PagedCost {
   double a, b;
   int32_t n;  // row blocks
   // (a product of one rounding, so that every caller gets the same number)
-  BS_HD int64_t start(int32_t i) const { return (int64_t)__builtin_floor(i * __builtin_fma((double)i, b, a)); }
+  BS_HD int32_t start(int32_t i) const { return (int32_t)(i * __builtin_fma((double)i, b, a)); }
   // The row block that slot y of the segment belongs to.
-  BS_HD int32_t find(int64_t y) const {
+  BS_HD int32_t find(int32_t y) const {
+    if (n == 1) return 0;
     double g = b > 0 ? (__builtin_sqrt(a * a + 4 * b * (double)y) - a) / (2 * b) : (double)y / a;
     int32_t i = g < n ? (int32_t)g : n - 1;
     while (i > 0 && start(i) > y) --i;
@@ -73,17 +74,28 @@ BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
   return c;
 }
 
-// Workgroups' ranges of a line of `all` slots: `per` slots each, `active` of them not empty.
+// Workgroups' ranges of a line of `all` places: `per` each (at least `least`), `active` of them not empty.  A line
+// has less than 2^31 places per KV head and less than 2^31 times the grid in all: the entry point refuses more.
 struct PagedRanges {
-  int64_t all, per;
-  int32_t active;
+  int64_t all;
+  int32_t per, active;
 };
-BS_HD PagedRanges paged_ranges(int64_t all, int32_t grid) {
+BS_HD PagedRanges paged_ranges(int64_t all, int32_t grid, int32_t least) {
   PagedRanges r;
   r.all = all;
-  r.per = all > grid ? (all + grid - 1) / grid : 1;
-  r.active = (int32_t)((all + r.per - 1) / r.per);
+  // (a quotient in float64 is off by one at most here)
+  int64_t per = (int64_t)((double)(all + grid - 1) / (double)grid);
+  if (per * grid < all) ++per;
+  if (per < least) per = least;
+  r.per = (int32_t)per;
+  r.active = (int32_t)((double)(all + per - 1) / (double)per);
+  while ((int64_t)r.active * per < all) ++r.active;
+  while (r.active > 0 && (int64_t)(r.active - 1) * per >= all) --r.active;
   return r;
+}
+// Ranges that share a row block of v places whose first lies `at` places into its range.
+BS_HD int32_t paged_pieces(int32_t at, int32_t v, int32_t per) {
+  return (int32_t)(((uint32_t)at + (uint32_t)v - 1) / (uint32_t)per) + 1;
 }
 // Range of block b of the grid: blocks are dealt to the 8 XCDs in turn, and each XCD takes neighbouring
 // ranges, which read the same keys.  -1: none.

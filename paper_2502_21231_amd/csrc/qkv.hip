@@ -46,20 +46,24 @@ struct RopeParams {
   int32_t num_seqs, max_pages, page_shift;
 };
 
-// Four consecutive elements, as float.
-__device__ __forceinline__ f32x4 load4(const bf16* p) {
-  const bf16x4 x = *reinterpret_cast<const bf16x4*>(p);
-  return f32x4{bf2f(x[0]), bf2f(x[1]), bf2f(x[2]), bf2f(x[3])};
-}
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+// Four consecutive elements, as they are in memory and as float.
+template <typename T> struct Four;
+template <> struct Four<bf16> { typedef bf16x4 type; };
+template <> struct Four<float> { typedef f32x4 type; };
+__device__ __forceinline__ f32x4 wide(bf16x4 x) { return f32x4{bf2f(x[0]), bf2f(x[1]), bf2f(x[2]), bf2f(x[3])}; }
+__device__ __forceinline__ f32x4 wide(f32x4 x) { return x; }
 __device__ __forceinline__ void store4(bf16* p, f32x4 x) {
   *reinterpret_cast<bf16x4*>(p) = bf16x4{f2bf(x[0]), f2bf(x[1]), f2bf(x[2]), f2bf(x[3])};
 }
 __device__ __forceinline__ void store4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 
-// The lane's eight elements of a head: pairs (a[e], b[e]).
+// The lane's eight elements of a head: pairs (a[e], b[e]); as loaded, its two runs of four.
 struct Pairs {
   f32x4 a, b;
+};
+template <typename T>
+struct Runs {
+  typename Four<T>::type a, b;
 };
 
 template <int D, bool kInter>
@@ -82,8 +86,13 @@ struct Lane {
     }
   }
   template <typename T>
-  __device__ __forceinline__ Pairs load(const T* row) const {
-    const f32x4 x = load4(row + ca), y = load4(row + cb);
+  __device__ __forceinline__ Runs<T> load(const T* row) const {
+    typedef typename Four<T>::type V;
+    return {*reinterpret_cast<const V*>(row + ca), *reinterpret_cast<const V*>(row + cb)};
+  }
+  template <typename T>
+  __device__ __forceinline__ static Pairs pairs(const Runs<T>& r) {
+    const f32x4 x = wide(r.a), y = wide(r.b);
     if (kInter) return {f32x4{x[0], x[2], y[0], y[2]}, f32x4{x[1], x[3], y[1], y[3]}};
     return {x, y};
   }
@@ -97,23 +106,20 @@ struct Lane {
       store4(row + cb, p.b);
     }
   }
-  __device__ __forceinline__ Pairs weight(const void* w, int is_f32) const {
-    Pairs p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int ia = kInter ? ca + 2 * e : ca + e, ib = kInter ? ca + 2 * e + 1 : cb + e;
-      p.a[e] = is_f32 ? static_cast<const float*>(w)[ia] : bf2f(static_cast<const bf16*>(w)[ia]);
-      p.b[e] = is_f32 ? static_cast<const float*>(w)[ib] : bf2f(static_cast<const bf16*>(w)[ib]);
-    }
-    return p;
-  }
 };
 
-// Sum over the N lanes (a power of two up to 16) of a row; every lane gets the same bits.
+// Sum over the N lanes (8 or 16 of a row of lanes) of a head; every lane gets the same bits.  Exchanges inside
+// a row of 16 lanes are operands of the additions, not LDS traffic as a shuffle is.
+template <int kCtrl>
+__device__ __forceinline__ float row_move(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, true));
+}
 template <int N>
 __device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-  for (int off = 1; off < N; off <<= 1) x += __shfl_xor(x, off);
+  x += row_move<0xB1>(x);   // quad_perm 1 0 3 2
+  x += row_move<0x4E>(x);   // quad_perm 2 3 0 1
+  x += row_move<0x141>(x);  // lane 7 - i of each 8
+  if constexpr (N == 16) x += row_move<0x140>(x);  // lane 15 - i
   return x;
 }
 
@@ -139,117 +145,174 @@ __device__ __forceinline__ void angles(const RopeParams& p, int64_t t, float* cs
   }
 }
 
-// One workgroup per token.  kAppend: keys and values into the cache, positions from its lengths.
+// The norms' weights as float in LDS (256 threads): the query's, then the key's.
+template <int D>
+__device__ __forceinline__ void stage_weights(const RopeParams& p, float* wt) {
+  const int i = threadIdx.x / D, e = threadIdx.x % D;
+  const void* w = i == 0 ? p.wq : p.wk;
+  if (i < 2 && w != nullptr)
+    wt[threadIdx.x] = p.w_f32 ? static_cast<const float*>(w)[e] : bf2f(static_cast<const bf16*>(w)[e]);
+}
+
+// The last b with cu_q[b] <= tok, by the lanes of a wave: 64 places at a time.
+__device__ __forceinline__ int sequence_of(const int32_t* cu_q, int n, int64_t tok) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;  // among entries lo .. lo + len - 1
+  while (len > 1) {
+    const int step = (len + 63) >> 6, i = lane * step;
+    const uint64_t m = __ballot(i < len && cu_q[lo + min(i, len - 1)] <= tok);
+    const int k = m == 0 ? 0 : 63 - __clzll(m);
+    lo += k * step;
+    len = min(step, len - k * step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// A workgroup takes tokens blockIdx.x, + gridDim.x, ...; its rows of D/8 lanes take kRows heads at a time, all
+// of them requested before the first is used.  kAppend: keys and values into the cache, positions from its
+// lengths (a token per workgroup).
+constexpr int kRows = 4;
+constexpr int kRopeFwdBlocks = 2048;  // eight per CU
+
 template <typename T, int D, bool kInter, bool kAppend>
 __global__ __launch_bounds__(256) void rope_fwd_kernel(const RopeParams p) {
-  constexpr int LPR = D / 8, ROWS = 256 / LPR;
-  __shared__ __attribute__((aligned(16))) float cs[D / 2], sn[D / 2];
-  const int tid = threadIdx.x, l = tid % LPR;
-  const int64_t tok = blockIdx.x;
-  int64_t t;
-  T* kd = nullptr;  // the token's place in the cache (head 0)
-  T* vd = nullptr;
-  if constexpr (kAppend) {
-    // the sequence of the token: the last b with cu_q[b] <= tok (empty ones skipped)
-    int lo = 0, hi = p.num_seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (p.cu_q[mid] <= tok) lo = mid; else hi = mid - 1;
-    }
-    const int64_t first = p.cu_q[lo], end = p.cu_q[lo + 1];
-    if (tok < first || tok >= end) return;  // behind the last sequence
-    t = p.kv_lens[lo] - end + tok;
-    const int64_t pg = t >> p.page_shift;
-    if (t >= 0 && pg < p.max_pages) {
-      const int64_t page = p.table[lo * p.table_stride + pg];
-      if (page >= 0 && page < p.num_pages) {
-        const int64_t at = page * p.page_stride + (t - (pg << p.page_shift)) * p.token_stride;
-        kd = reinterpret_cast<T*>(p.kc) + at;
-        vd = reinterpret_cast<T*>(p.vc) + at;
-      }
-    }
-  } else {
-    t = p.pos[tok];
-  }
-  angles(p, t, cs, sn);
-  __syncthreads();
+  constexpr int LPR = D / 8, ROWS = 256 / LPR, E = 16 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) float cs[2][D / 2], sn[2][D / 2];
+  __shared__ __attribute__((aligned(16))) float wt[2 * D];
+  const int tid = threadIdx.x, l = tid % LPR, row = tid / LPR;
   const Lane<D, kInter> lane(l, p.rot);
-  f32x4 c = f32x4{}, s = f32x4{};
-  if (lane.turned) {
-    c = *reinterpret_cast<const f32x4*>(cs + lane.f0);
-    s = *reinterpret_cast<const f32x4*>(sn + lane.f0);
-  }
-  const T* q = static_cast<const T*>(p.q.p) + tok * p.q.stride;
-  const T* k = static_cast<const T*>(p.k.p) + tok * p.k.stride;
-  const int nq = p.q.p != nullptr ? p.hq : 0;
-  for (int h = tid / LPR; h < nq + p.hkv; h += ROWS) {
-    const bool is_q = h < nq;
-    T* dst = is_q ? static_cast<T*>(p.q_out) + (tok * p.hq + h) * D
-                  : (kAppend ? (kd != nullptr ? kd + (h - nq) * p.head_stride : nullptr)
-                             : static_cast<T*>(p.k_out) + (tok * p.hkv + h - nq) * D);
-    if (kAppend && dst == nullptr) continue;
-    Pairs x = lane.load(is_q ? q + h * D : k + (h - nq) * D);
-    const void* w = is_q ? p.wq : p.wk;
-    if (w != nullptr) {
-      const float r = rsqrtf(row_sum<LPR>(dot(x, x)) * (1.f / D) + p.eps);
-      const Pairs wt = lane.weight(w, p.w_f32);
-      x.a *= wt.a * r;
-      x.b *= wt.b * r;
+  const int nq = p.q.p != nullptr ? p.hq : 0, n = nq + p.hkv;
+  stage_weights<D>(p, wt);
+  int buf = 0;
+  for (int64_t tok = blockIdx.x; tok < p.tokens; tok += gridDim.x, buf ^= 1) {
+    const T* q = static_cast<const T*>(p.q.p) + tok * p.q.stride;
+    const T* k = static_cast<const T*>(p.k.p) + tok * p.k.stride;
+    Runs<T> in[kRows];
+    auto request = [&](int h0) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int h = h0 + i * ROWS;
+        if (h < n) in[i] = lane.load(h < nq ? q + h * D : k + (h - nq) * D);
+      }
+    };
+    request(row);
+    int64_t t;
+    T* kd = nullptr;  // the token's place in the cache (head 0)
+    T* vd = nullptr;
+    if constexpr (kAppend) {
+      const int b = sequence_of(p.cu_q, p.num_seqs, tok);
+      const int64_t first = p.cu_q[b], end = p.cu_q[b + 1];
+      if (tok < first || tok >= end) continue;  // behind the last sequence
+      t = p.kv_lens[b] - end + tok;
+      const int64_t pg = t >> p.page_shift;
+      if (t >= 0 && pg < p.max_pages) {
+        const int64_t page = p.table[b * p.table_stride + pg];
+        if (page >= 0 && page < p.num_pages) {
+          const int64_t at = page * p.page_stride + (t - (pg << p.page_shift)) * p.token_stride;
+          kd = reinterpret_cast<T*>(p.kc) + at;
+          vd = reinterpret_cast<T*>(p.vc) + at;
+        }
+      }
+    } else {
+      t = p.pos[tok];
     }
-    if (lane.turned) turn(x, c, s);
-    lane.store(dst, x);
-  }
-  if constexpr (kAppend) {
-    if (vd == nullptr) return;
-    const T* v = static_cast<const T*>(p.v.p) + tok * p.v.stride;
-    constexpr int E = 16 / sizeof(T);  // bits as they are
-    for (int u = tid; u < p.hkv * (D / E); u += 256) {
-      const int h = u / (D / E), e = u % (D / E) * E;
-      *reinterpret_cast<u32x4*>(vd + h * p.head_stride + e) = *reinterpret_cast<const u32x4*>(v + h * D + e);
+    angles(p, t, cs[buf], sn[buf]);
+    __syncthreads();
+    f32x4 c = f32x4{}, s = f32x4{};
+    if (lane.turned) {
+      c = *reinterpret_cast<const f32x4*>(cs[buf] + lane.f0);
+      s = *reinterpret_cast<const f32x4*>(sn[buf] + lane.f0);
+    }
+    for (int h0 = row; h0 < n; h0 += kRows * ROWS) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int h = h0 + i * ROWS;
+        if (h >= n) break;
+        const bool is_q = h < nq;
+        T* dst = is_q ? static_cast<T*>(p.q_out) + (tok * p.hq + h) * D
+                      : (kAppend ? (kd != nullptr ? kd + (h - nq) * p.head_stride : nullptr)
+                                 : static_cast<T*>(p.k_out) + (tok * p.hkv + h - nq) * D);
+        if (kAppend && dst == nullptr) break;
+        Pairs x = lane.pairs(in[i]);
+        if ((is_q ? p.wq : p.wk) != nullptr) {
+          const float r = rsqrtf(row_sum<LPR>(dot(x, x)) * (1.f / D) + p.eps);
+          const float* w = wt + (is_q ? 0 : D);
+          const Pairs g = lane.pairs(lane.load(w));
+          x.a *= g.a * r;
+          x.b *= g.b * r;
+        }
+        if (lane.turned) turn(x, c, s);
+        lane.store(dst, x);
+      }
+      request(h0 + kRows * ROWS);
+    }
+    if constexpr (kAppend) {
+      if (vd == nullptr) continue;
+      const T* v = static_cast<const T*>(p.v.p) + tok * p.v.stride;
+      for (int u = tid; u < p.hkv * (D / E); u += 256) {  // bits as they are
+        const int h = u / (D / E), e = u % (D / E) * E;
+        *reinterpret_cast<u32x4*>(vd + h * p.head_stride + e) = *reinterpret_cast<const u32x4*>(v + h * D + e);
+      }
     }
   }
 }
 
 template <typename T, int D, bool kInter>
 __global__ __launch_bounds__(256) void rope_bwd_kernel(const RopeParams p) {
-  constexpr int LPR = D / 8, ROWS = 256 / LPR;
-  __shared__ __attribute__((aligned(16))) float cs[D / 2], sn[D / 2];
+  constexpr int LPR = D / 8, ROWS = 256 / LPR, U = 2;  // heads requested together
+  __shared__ __attribute__((aligned(16))) float cs[2][D / 2], sn[2][D / 2];
+  __shared__ __attribute__((aligned(16))) float wt[2 * D];
   __shared__ __attribute__((aligned(16))) float acc[ROWS][D];
   const int tid = threadIdx.x, l = tid % LPR, row = tid / LPR;
   const Lane<D, kInter> lane(l, p.rot);
   Pairs dw[2] = {{f32x4{}, f32x4{}}, {f32x4{}, f32x4{}}};  // of the query's weight and the key's
-  for (int64_t tok = blockIdx.x; tok < p.tokens; tok += gridDim.x) {
-    __syncthreads();
-    angles(p, p.pos[tok], cs, sn);
+  stage_weights<D>(p, wt);
+  int buf = 0;
+  for (int64_t tok = blockIdx.x; tok < p.tokens; tok += gridDim.x, buf ^= 1) {
+    angles(p, p.pos[tok], cs[buf], sn[buf]);
     __syncthreads();
     f32x4 c = f32x4{}, s = f32x4{};
     if (lane.turned) {
-      c = *reinterpret_cast<const f32x4*>(cs + lane.f0);
-      s = *reinterpret_cast<const f32x4*>(sn + lane.f0);
+      c = *reinterpret_cast<const f32x4*>(cs[buf] + lane.f0);
+      s = *reinterpret_cast<const f32x4*>(sn[buf] + lane.f0);
     }
-    auto heads = [&](const Heads& x, const void* g, const Heads& dx, int n, const void* w, Pairs& dwx) {
-      const Pairs wt = w != nullptr ? lane.weight(w, p.w_f32) : Pairs{f32x4{}, f32x4{}};
-      for (int h = row; h < n; h += ROWS) {
-        Pairs y = lane.load(static_cast<const T*>(g) + (tok * n + h) * D);
-        if (lane.turned) turn(y, c, -s);
-        if (w != nullptr) {
-          Pairs xx = lane.load(static_cast<const T*>(x.p) + tok * x.stride + h * D);
-          const float r = rsqrtf(row_sum<LPR>(dot(xx, xx)) * (1.f / D) + p.eps);
-          xx.a *= r;
-          xx.b *= r;
-          dwx.a += y.a * xx.a;
-          dwx.b += y.b * xx.b;
-          y.a *= wt.a;
-          y.b *= wt.b;
-          const float m = row_sum<LPR>(dot(y, xx)) * (1.f / D);
-          y.a = (y.a - xx.a * m) * r;
-          y.b = (y.b - xx.b * m) * r;
+    auto heads = [&](const Heads& x, const void* g, const Heads& dx, int n, bool norm, const float* w, Pairs& dwx) {
+      for (int h0 = row; h0 < n; h0 += U * ROWS) {
+        Runs<T> gi[U], xi[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int h = h0 + i * ROWS;
+          if (h < n) {
+            gi[i] = lane.load(static_cast<const T*>(g) + (tok * n + h) * D);
+            if (norm) xi[i] = lane.load(static_cast<const T*>(x.p) + tok * x.stride + h * D);
+          }
         }
-        lane.store(static_cast<T*>(dx.p) + tok * dx.stride + h * D, y);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int h = h0 + i * ROWS;
+          if (h >= n) break;
+          Pairs y = lane.pairs(gi[i]);
+          if (lane.turned) turn(y, c, -s);
+          if (norm) {
+            Pairs xx = lane.pairs(xi[i]);
+            const float r = rsqrtf(row_sum<LPR>(dot(xx, xx)) * (1.f / D) + p.eps);
+            xx.a *= r;
+            xx.b *= r;
+            dwx.a += y.a * xx.a;
+            dwx.b += y.b * xx.b;
+            const Pairs wg = lane.pairs(lane.load(w));
+            y.a *= wg.a;
+            y.b *= wg.b;
+            const float m = row_sum<LPR>(dot(y, xx)) * (1.f / D);
+            y.a = (y.a - xx.a * m) * r;
+            y.b = (y.b - xx.b * m) * r;
+          }
+          lane.store(static_cast<T*>(dx.p) + tok * dx.stride + h * D, y);
+        }
       }
     };
-    heads(p.q, p.gq, p.dq, p.hq, p.wq, dw[0]);
-    heads(p.k, p.gk, p.dk, p.hkv, p.wk, dw[1]);
+    heads(p.q, p.gq, p.dq, p.hq, p.wq != nullptr, wt, dw[0]);
+    heads(p.k, p.gk, p.dk, p.hkv, p.wk != nullptr, wt + D, dw[1]);
   }
   if (p.part == nullptr) return;
   for (int i = 0; i < 2; ++i) {
@@ -319,7 +382,7 @@ hipError_t launch_qk_rope_fwd(const bs_dims& d, const bs_qk_params& P, Heads q, 
   p.k = k;
   p.q_out = q_out;
   p.k_out = k_out;
-  const dim3 grid((unsigned)d.total_q);
+  const dim3 grid((unsigned)(d.total_q < kRopeFwdBlocks ? d.total_q : kRopeFwdBlocks));
 #define BS_CALL(T, D, I) hipLaunchKernelGGL((rope_fwd_kernel<T, D, I, false>), grid, dim3(256), 0, stream, p)
   BS_ROPE_DISPATCH(BS_CALL);
 #undef BS_CALL

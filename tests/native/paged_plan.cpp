@@ -22,6 +22,7 @@ using namespace bs;
   } while (0)
 
 static void segment(const PagedSeg& s, int BM, int BLK) {
+  if ((double)paged_row_blocks(s, BM) * (s.lk / BLK + 3) >= 2147483648.0) return;  // (no line)
   const PagedCost c = paged_cost(s, BM, BLK);
   CHECK(c.n == paged_row_blocks(s, BM));
   CHECK(c.start(0) == 0);
@@ -41,15 +42,19 @@ static void segment(const PagedSeg& s, int BM, int BLK) {
   if (c.n == 1) CHECK(c.start(1) == need);
 }
 
-static void line(const std::vector<PagedSeg>& segs, int hkv, int BM, int BLK, int grid) {
+// Segments of up to 32 rows take the first shape, others the second.
+static void line(const std::vector<PagedSeg>& segs, int hkv, int grid, int least) {
+  const int bm[2] = {32, 128}, blk[2] = {128, 64};
+  auto kind = [&](const PagedSeg& s) { return (int64_t)s.lq * s.group <= 32 ? 0 : 1; };
   int64_t per_head = 0;
   std::vector<int64_t> pre;
   for (const PagedSeg& s : segs) {
     pre.push_back(per_head);
-    if (s.lq > 0) per_head += paged_cost(s, BM, BLK).start(paged_row_blocks(s, BM));
+    const int t = kind(s);
+    if (s.lq > 0) per_head += paged_cost(s, bm[t], blk[t]).start(paged_row_blocks(s, bm[t]));
   }
-  const PagedRanges R = paged_ranges(per_head * hkv, grid);
-  CHECK(R.active <= grid && R.active * R.per >= R.all && (R.active == 0 || (R.active - 1) * R.per < R.all));
+  const PagedRanges R = paged_ranges(per_head * hkv, grid, least);
+  CHECK(R.active <= grid && R.active * (int64_t)R.per >= R.all && (R.active == 0 || (R.active - 1) * (int64_t)R.per < R.all));
   std::vector<int> taken(grid, 0);
   for (int32_t b = 0; b < grid; ++b) {
     const int32_t w = paged_range_of(b, R.active);
@@ -57,21 +62,24 @@ static void line(const std::vector<PagedSeg>& segs, int hkv, int BM, int BLK, in
     if (w >= 0) CHECK(++taken[w] == 1);
   }
   for (int32_t w = 0; w < R.active; ++w) CHECK(taken[w] == 1);
+  std::vector<int> heads_of(R.active, 0), tails_of(R.active, 0);  // pieces that leave sums: one of each at most
   for (int h = 0; h < hkv; ++h)
     for (size_t b = 0; b < segs.size(); ++b) {
       if (segs[b].lq == 0) continue;
-      const PagedCost c = paged_cost(segs[b], BM, BLK);
+      const int t = kind(segs[b]);
+      const PagedCost c = paged_cost(segs[b], bm[t], blk[t]);
       for (int32_t i = 0; i < c.n; ++i) {
-        const int64_t xs = h * per_head + pre[b] + c.start(i), v = paged_blocks(segs[b], BM, BLK, i);
-        const int64_t first = xs / R.per, last = (xs + v - 1) / R.per;
-        int64_t seen = 0;
-        for (int64_t w = first; w <= last; ++w) {
-          const int64_t lo = std::max(w * R.per, xs), hi = std::min((w + 1) * R.per, xs + v);
-          CHECK(lo < hi && w < R.active);
-          if (w > first) CHECK(lo == w * R.per);  // the one piece of its range that goes on from another
-          seen += hi - lo;
+        const int64_t xs = h * per_head + pre[b] + c.start(i), first = xs / R.per;
+        const int32_t v = paged_blocks(segs[b], bm[t], blk[t], i);
+        const int32_t pieces = paged_pieces((int32_t)(xs - first * R.per), v, R.per);
+        int64_t done = 0;
+        for (int32_t k = 0; k < pieces; ++k) {
+          const int64_t w = first + k, lo = std::max(w * R.per, xs), hi = std::min((w + 1) * R.per, xs + v);
+          CHECK(w < R.active && lo - xs == done && hi > lo);
+          done += hi - lo;
+          if (pieces > 1) CHECK(++(lo == xs ? heads_of : tails_of)[w] == 1);
         }
-        CHECK(seen == v);
+        CHECK(done == v);
       }
     }
 }
@@ -100,8 +108,13 @@ int main() {
     std::vector<PagedSeg> segs(rng() % 20);
     const int32_t group = pick(1, 16), causal = rng() % 4 != 0;
     for (PagedSeg& s : segs) s = PagedSeg{(int32_t)(rng() % 5 ? pick(1, 300) : 0), pick(1, 3000) - 1, group, causal};
-    const int* t = tiles[n % 4];
-    line(segs, 1 + rng() % 9, t[0], t[1], n % 2 ? 512 : 8 * (1 + rng() % 64));
+    line(segs, 1 + rng() % 9, n % 2 ? 512 : 8 * (1 + rng() % 64), 1 + n % 5);
   }
+  for (int64_t all : {(int64_t)0, (int64_t)1, (int64_t)511, (int64_t)512, (int64_t)513, ((int64_t)1 << 39) - 1})
+    for (int n = 0; n < 2000; ++n) {
+      const PagedRanges R = paged_ranges(all - n * (all >> 12), 512, 1);
+      CHECK(R.per >= 1 && R.active * (int64_t)R.per >= R.all && (R.active == 0 || (R.active - 1) * (int64_t)R.per < R.all));
+      CHECK(R.active <= 512 && (R.per == 1 || (R.per - 1) * (int64_t)512 < R.all));
+    }
   std::puts("ok");
 }
