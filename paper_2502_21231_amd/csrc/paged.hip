@@ -427,7 +427,7 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
     for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 16);
   }
   const int full = seen_by(p, e, (int)((uint32_t)(e.rb * BM) / (uint32_t)p.group));
-  const int n_full = full > 0 ? full / BN : 0;
+  const int n_full = __builtin_amdgcn_readfirstlane(full > 0 ? full / BN : 0);  // tiles that all rows see whole
   const int t0 = e.kb, n_tiles = e.kb + e.n, keys = e.lk;
 
   const int32_t* table = p.table + e.seg * p.table_stride;
@@ -534,18 +534,15 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
     wait_vmem_all();
     __syncthreads();
   };
-  for (int t = t0;; t += 2) {
-    if (t + 1 == n_tiles) {
-      step(std::false_type{}, t, X, X + TILE, S.miss[0], Y, Y + TILE, S.miss[1]);
-      break;
-    }
+  int t = t0;
+  for (; t + 2 < n_tiles; t += 2) {
     step(std::true_type{}, t, X, X + TILE, S.miss[0], Y, Y + TILE, S.miss[1]);
-    if (t + 2 == n_tiles) {
-      step(std::false_type{}, t + 1, Y, Y + TILE, S.miss[1], X, X + TILE, S.miss[0]);
-      break;
-    }
     step(std::true_type{}, t + 1, Y, Y + TILE, S.miss[1], X, X + TILE, S.miss[0]);
   }
+  const bool two = t + 2 == n_tiles;
+  if (two) step(std::true_type{}, t, X, X + TILE, S.miss[0], Y, Y + TILE, S.miss[1]);
+  const bf16* Z = two ? Y : X;
+  step(std::false_type{}, n_tiles - 1, Z, Z + TILE, S.miss[two], nullptr, nullptr, nullptr);
 
   const float l_tot = half_sum(l_run);
   if (!qvalid) return;
