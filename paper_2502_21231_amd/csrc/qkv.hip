@@ -9,8 +9,9 @@
 //
 // A head is held by D/8 lanes of eight elements, four pairs of the rotation in each: pairs (i, i +
 // rot/2) are loaded as two runs of four elements from the two halves, so that no lane needs another's
-// elements (for the norm's sum a few exchanges among the D/8 lanes are left).  A workgroup takes a
-// token; its rows of lanes share the token's heads, and its angles, whose sines are taken once.
+// elements (for the norm's sum a few exchanges among the D/8 lanes are left).  A workgroup takes one, two or four
+// tokens at a time, so many that each of its rows of lanes has up to four heads to request at once; a
+// token's sines are taken once and shared through LDS.
 //
 // Angles: t f in float64, reduced to a part of a turn there; at t = 2M a float32 angle would be off
 // by up to 0.06.
@@ -44,6 +45,7 @@ struct RopeParams {
   const int32_t* kv_lens;
   const int32_t* cu_q;
   int32_t num_seqs, max_pages, page_shift;
+  int32_t together;       // tokens of a workgroup at a time: 1, 2 or 4
 };
 
 // Four consecutive elements, as they are in memory and as float.
@@ -136,9 +138,10 @@ __device__ __forceinline__ void turn(Pairs& x, f32x4 c, f32x4 s) {
   x.b = x.b * c + a * s;
 }
 
-// cos and sin of t f: f32 arrays in LDS, written by the workgroup's first rot / 2 threads.
+// cos and sin of t f of a wave's token in LDS, by the lanes below rot / 2 <= 64.
+template <int D>
 __device__ __forceinline__ void angles(const RopeParams& p, int64_t t, float* cs, float* sn) {
-  const int i = threadIdx.x;
+  const int i = threadIdx.x & 63;
   if (i < p.rot / 2) {
     const double turns = (double)t * ((double)p.freq[i] * 0.15915494309189533577);  // 1 / 2 pi
     sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
@@ -168,44 +171,63 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu_q, int n, int64_t t
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// A workgroup takes tokens blockIdx.x, + gridDim.x, ...; its rows of D/8 lanes take kRows heads at a time, all
-// of them requested before the first is used.  kAppend: keys and values into the cache, positions from its
-// lengths (a token per workgroup).
+// Rows of lanes of a workgroup by token: `together` tokens share them, whole waves each.
+struct Share {
+  int sub, row, rows;  // this thread's token, its row among that token's, and how many those are
+  bool first;          // whether its wave is the token's first
+  template <int ROWS>
+  static __device__ __forceinline__ Share of(int together, int row) {
+    const int per = ROWS / together;
+    Share s;
+    s.sub = __builtin_amdgcn_readfirstlane(row / per);
+    s.row = row - s.sub * per;
+    s.rows = per;
+    s.first = (threadIdx.x >> 6) * together % 4 == 0;
+    return s;
+  }
+};
+
+// A workgroup takes tokens n b .. n b + n - 1 of n = p.together, then those gridDim.x further; a row of D/8
+// lanes takes kRows heads at a time, all of them requested before the first is used.  kAppend: keys and
+// values into the cache, positions from its lengths.
 constexpr int kRows = 4;
 constexpr int kRopeFwdBlocks = 2048;  // eight per CU
 
 template <typename T, int D, bool kInter, bool kAppend>
 __global__ __launch_bounds__(256) void rope_fwd_kernel(const RopeParams p) {
   constexpr int LPR = D / 8, ROWS = 256 / LPR, E = 16 / sizeof(T);
-  __shared__ __attribute__((aligned(16))) float cs[2][D / 2], sn[2][D / 2];
+  __shared__ __attribute__((aligned(16))) float cs[2][4][D / 2], sn[2][4][D / 2];
   __shared__ __attribute__((aligned(16))) float wt[2 * D];
-  const int tid = threadIdx.x, l = tid % LPR, row = tid / LPR;
+  const int tid = threadIdx.x, l = tid % LPR;
   const Lane<D, kInter> lane(l, p.rot);
+  const Share sh = Share::of<ROWS>(p.together, tid / LPR);
   const int nq = p.q.p != nullptr ? p.hq : 0, n = nq + p.hkv;
   stage_weights<D>(p, wt);
   int buf = 0;
-  for (int64_t tok = blockIdx.x; tok < p.tokens; tok += gridDim.x, buf ^= 1) {
+  for (int64_t t0 = (int64_t)blockIdx.x * p.together; t0 < p.tokens; t0 += (int64_t)gridDim.x * p.together, buf ^= 1) {
+    const int64_t tok = t0 + sh.sub;
+    bool live = tok < p.tokens;
     const T* q = static_cast<const T*>(p.q.p) + tok * p.q.stride;
     const T* k = static_cast<const T*>(p.k.p) + tok * p.k.stride;
     Runs<T> in[kRows];
     auto request = [&](int h0) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
-        const int h = h0 + i * ROWS;
-        if (h < n) in[i] = lane.load(h < nq ? q + h * D : k + (h - nq) * D);
+        const int h = h0 + i * sh.rows;
+        if (live && h < n) in[i] = lane.load(h < nq ? q + h * D : k + (h - nq) * D);
       }
     };
-    request(row);
-    int64_t t;
+    request(sh.row);
+    int64_t t = 0;
     T* kd = nullptr;  // the token's place in the cache (head 0)
     T* vd = nullptr;
     if constexpr (kAppend) {
       const int b = sequence_of(p.cu_q, p.num_seqs, tok);
       const int64_t first = p.cu_q[b], end = p.cu_q[b + 1];
-      if (tok < first || tok >= end) continue;  // behind the last sequence
+      live = live && tok >= first && tok < end;  // (no token, or behind the last sequence)
       t = p.kv_lens[b] - end + tok;
       const int64_t pg = t >> p.page_shift;
-      if (t >= 0 && pg < p.max_pages) {
+      if (live && t >= 0 && pg < p.max_pages) {
         const int64_t page = p.table[b * p.table_stride + pg];
         if (page >= 0 && page < p.num_pages) {
           const int64_t at = page * p.page_stride + (t - (pg << p.page_shift)) * p.token_stride;
@@ -213,20 +235,20 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(const RopeParams p) {
           vd = reinterpret_cast<T*>(p.vc) + at;
         }
       }
-    } else {
+    } else if (live) {
       t = p.pos[tok];
     }
-    angles(p, t, cs[buf], sn[buf]);
+    if (sh.first) angles<D>(p, t, cs[buf][sh.sub], sn[buf][sh.sub]);
     __syncthreads();
     f32x4 c = f32x4{}, s = f32x4{};
     if (lane.turned) {
-      c = *reinterpret_cast<const f32x4*>(cs[buf] + lane.f0);
-      s = *reinterpret_cast<const f32x4*>(sn[buf] + lane.f0);
+      c = *reinterpret_cast<const f32x4*>(cs[buf][sh.sub] + lane.f0);
+      s = *reinterpret_cast<const f32x4*>(sn[buf][sh.sub] + lane.f0);
     }
-    for (int h0 = row; h0 < n; h0 += kRows * ROWS) {
+    for (int h0 = sh.row; live && h0 < n; h0 += kRows * sh.rows) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
-        const int h = h0 + i * ROWS;
+        const int h = h0 + i * sh.rows;
         if (h >= n) break;
         const bool is_q = h < nq;
         T* dst = is_q ? static_cast<T*>(p.q_out) + (tok * p.hq + h) * D
@@ -244,12 +266,13 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(const RopeParams p) {
         if (lane.turned) turn(x, c, s);
         lane.store(dst, x);
       }
-      request(h0 + kRows * ROWS);
+      request(h0 + kRows * sh.rows);
     }
     if constexpr (kAppend) {
       if (vd == nullptr) continue;
       const T* v = static_cast<const T*>(p.v.p) + tok * p.v.stride;
-      for (int u = tid; u < p.hkv * (D / E); u += 256) {  // bits as they are
+      const int mine = 256 / p.together;
+      for (int u = tid & (mine - 1); u < p.hkv * (D / E); u += mine) {  // bits as they are
         const int h = u / (D / E), e = u % (D / E) * E;
         *reinterpret_cast<u32x4*>(vd + h * p.head_stride + e) = *reinterpret_cast<const u32x4*>(v + h * D + e);
       }
@@ -260,64 +283,79 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(const RopeParams p) {
 template <typename T, int D, bool kInter>
 __global__ __launch_bounds__(256) void rope_bwd_kernel(const RopeParams p) {
   constexpr int LPR = D / 8, ROWS = 256 / LPR, U = 2;  // heads requested together
-  __shared__ __attribute__((aligned(16))) float cs[2][D / 2], sn[2][D / 2];
+  __shared__ __attribute__((aligned(16))) float cs[2][4][D / 2], sn[2][4][D / 2];
   __shared__ __attribute__((aligned(16))) float wt[2 * D];
   __shared__ __attribute__((aligned(16))) float acc[ROWS][D];
   const int tid = threadIdx.x, l = tid % LPR, row = tid / LPR;
   const Lane<D, kInter> lane(l, p.rot);
-  Pairs dw[2] = {{f32x4{}, f32x4{}}, {f32x4{}, f32x4{}}};  // of the query's weight and the key's
+  const Share sh = Share::of<ROWS>(p.together, row);
+  const int n = p.hq + p.hkv;
+  Pairs dwq = {f32x4{}, f32x4{}}, dwk = {f32x4{}, f32x4{}};
   stage_weights<D>(p, wt);
   int buf = 0;
-  for (int64_t tok = blockIdx.x; tok < p.tokens; tok += gridDim.x, buf ^= 1) {
-    angles(p, p.pos[tok], cs[buf], sn[buf]);
-    __syncthreads();
-    f32x4 c = f32x4{}, s = f32x4{};
-    if (lane.turned) {
-      c = *reinterpret_cast<const f32x4*>(cs[buf] + lane.f0);
-      s = *reinterpret_cast<const f32x4*>(sn[buf] + lane.f0);
-    }
-    auto heads = [&](const Heads& x, const void* g, const Heads& dx, int n, bool norm, const float* w, Pairs& dwx) {
-      for (int h0 = row; h0 < n; h0 += U * ROWS) {
-        Runs<T> gi[U], xi[U];
+  for (int64_t t0 = (int64_t)blockIdx.x * p.together; t0 < p.tokens; t0 += (int64_t)gridDim.x * p.together, buf ^= 1) {
+    const int64_t tok = t0 + sh.sub;
+    const bool live = tok < p.tokens;
+    Runs<T> gi[U], xi[U];
+    auto request = [&](int h0) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int h = h0 + i * ROWS;
-          if (h < n) {
-            gi[i] = lane.load(static_cast<const T*>(g) + (tok * n + h) * D);
-            if (norm) xi[i] = lane.load(static_cast<const T*>(x.p) + tok * x.stride + h * D);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int h = h0 + i * ROWS;
-          if (h >= n) break;
-          Pairs y = lane.pairs(gi[i]);
-          if (lane.turned) turn(y, c, -s);
-          if (norm) {
-            Pairs xx = lane.pairs(xi[i]);
-            const float r = rsqrtf(row_sum<LPR>(dot(xx, xx)) * (1.f / D) + p.eps);
-            xx.a *= r;
-            xx.b *= r;
-            dwx.a += y.a * xx.a;
-            dwx.b += y.b * xx.b;
-            const Pairs wg = lane.pairs(lane.load(w));
-            y.a *= wg.a;
-            y.b *= wg.b;
-            const float m = row_sum<LPR>(dot(y, xx)) * (1.f / D);
-            y.a = (y.a - xx.a * m) * r;
-            y.b = (y.b - xx.b * m) * r;
-          }
-          lane.store(static_cast<T*>(dx.p) + tok * dx.stride + h * D, y);
+      for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * sh.rows;
+        if (!live || h >= n) continue;
+        const bool is_q = h < p.hq;
+        const int hh = is_q ? h : h - p.hq;
+        gi[i] = lane.load(static_cast<const T*>(is_q ? p.gq : p.gk) + (tok * (is_q ? p.hq : p.hkv) + hh) * D);
+        if ((is_q ? p.wq : p.wk) != nullptr) {
+          const Heads& x = is_q ? p.q : p.k;
+          xi[i] = lane.load(static_cast<const T*>(x.p) + tok * x.stride + hh * D);
         }
       }
     };
-    heads(p.q, p.gq, p.dq, p.hq, p.wq != nullptr, wt, dw[0]);
-    heads(p.k, p.gk, p.dk, p.hkv, p.wk != nullptr, wt + D, dw[1]);
+    request(sh.row);
+    if (sh.first && live) angles<D>(p, p.pos[tok], cs[buf][sh.sub], sn[buf][sh.sub]);
+    __syncthreads();
+    f32x4 c = f32x4{}, s = f32x4{};
+    if (lane.turned) {
+      c = *reinterpret_cast<const f32x4*>(cs[buf][sh.sub] + lane.f0);
+      s = *reinterpret_cast<const f32x4*>(sn[buf][sh.sub] + lane.f0);
+    }
+    for (int h0 = sh.row; live && h0 < n; h0 += U * sh.rows) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * sh.rows;
+        if (h >= n) break;
+        const bool is_q = h < p.hq;
+        Pairs y = lane.pairs(gi[i]);
+        if (lane.turned) turn(y, c, -s);
+        if ((is_q ? p.wq : p.wk) != nullptr) {
+          Pairs xx = lane.pairs(xi[i]);
+          const float r = rsqrtf(row_sum<LPR>(dot(xx, xx)) * (1.f / D) + p.eps);
+          xx.a *= r;
+          xx.b *= r;
+          if (is_q) {
+            dwq.a += y.a * xx.a;
+            dwq.b += y.b * xx.b;
+          } else {
+            dwk.a += y.a * xx.a;
+            dwk.b += y.b * xx.b;
+          }
+          const Pairs wg = lane.pairs(lane.load(static_cast<const float*>(wt + (is_q ? 0 : D))));
+          y.a *= wg.a;
+          y.b *= wg.b;
+          const float m = row_sum<LPR>(dot(y, xx)) * (1.f / D);
+          y.a = (y.a - xx.a * m) * r;
+          y.b = (y.b - xx.b * m) * r;
+        }
+        const Heads& dx = is_q ? p.dq : p.dk;
+        lane.store(static_cast<T*>(dx.p) + tok * dx.stride + (is_q ? h : h - p.hq) * D, y);
+      }
+      request(h0 + U * sh.rows);
+    }
   }
   if (p.part == nullptr) return;
   for (int i = 0; i < 2; ++i) {
     __syncthreads();
-    lane.store(acc[row], dw[i]);
+    lane.store(acc[row], i == 0 ? dwq : dwk);
     __syncthreads();
     for (int e = tid; e < D; e += 256) {
       float s = 0.f;
@@ -327,21 +365,27 @@ __global__ __launch_bounds__(256) void rope_bwd_kernel(const RopeParams p) {
   }
 }
 
-// dw[i][e] = sum over blocks of part[block][i][e]; one workgroup per (i, 16 elements).
-__global__ __launch_bounds__(256) void rope_dw_kernel(const float* __restrict__ part, int blocks, int D,
-                                                      float* dwq, float* dwk) {
-  __shared__ float acc[16][17];
-  const int e = threadIdx.x & 15, j = threadIdx.x >> 4;
-  const int col = blockIdx.x * 16 + e;
-  float s = 0.f;
-  for (int b = j; b < blocks; b += 16) s += part[(int64_t)b * 2 * D + col];
+// dw[i][e] = sum over blocks of part[block][i][e]; one workgroup per 16 of the 2 D columns, four of them to a lane
+// and the blocks dealt to its 256 rows of four lanes.
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const float* __restrict__ part, int blocks, int D,
+                                                       float* dwq, float* dwk) {
+  __shared__ __attribute__((aligned(16))) f32x4 acc[256][4];
+  const int e = threadIdx.x & 3, j = threadIdx.x >> 2;
+  const float* src = part + blockIdx.x * 16 + e * 4;
+  f32x4 s = f32x4{};
+#pragma unroll
+  for (int i = 0; i < kRopeBwdBlocks / 256; ++i)
+    if (j + i * 256 < blocks) s += *reinterpret_cast<const f32x4*>(src + (int64_t)(j + i * 256) * 2 * D);
   acc[j][e] = s;
-  __syncthreads();
+  for (int half = 128; half > 0; half >>= 1) {
+    __syncthreads();
+    if (j < half) acc[j][e] += acc[j + half][e];
+  }
   if (j != 0) return;
-  s = 0.f;
-  for (int i = 0; i < 16; ++i) s += acc[i][e];
+  const int col = blockIdx.x * 16 + e * 4;
   float* out = col < D ? dwq : dwk;
-  if (out != nullptr) out[col < D ? col : col - D] = s;
+  if (out == nullptr) return;
+  for (int i = 0; i < 4; ++i) out[(col < D ? col : col - D) + i] = acc[0][e][i];
 }
 
 RopeParams params_of(const bs_dims& d, const bs_qk_params& P) {
@@ -356,6 +400,15 @@ RopeParams params_of(const bs_dims& d, const bs_qk_params& P) {
   p.hq = d.hq;
   p.hkv = d.hkv;
   return p;
+}
+
+// Tokens that a workgroup takes at a time: as many (1, 2 or 4) as give each row of lanes up to `heads` heads, and no
+// more than leave every CU eight workgroups.
+int together_of(const bs_dims& d, int heads, int n) {
+  const int rows = 256 / (d.head_dim / 8) * heads;
+  int t = 1;
+  while (t < 4 && 2 * t * n <= rows && d.total_q >= 2048 * 2 * t) t *= 2;
+  return t;
 }
 
 // Calls F<T, D, kInter> with the types of the call.
@@ -382,7 +435,9 @@ hipError_t launch_qk_rope_fwd(const bs_dims& d, const bs_qk_params& P, Heads q, 
   p.k = k;
   p.q_out = q_out;
   p.k_out = k_out;
-  const dim3 grid((unsigned)(d.total_q < kRopeFwdBlocks ? d.total_q : kRopeFwdBlocks));
+  p.together = together_of(d, kRows, d.hq + d.hkv);
+  const int64_t blocks = (d.total_q + p.together - 1) / p.together;
+  const dim3 grid((unsigned)(blocks < kRopeFwdBlocks ? blocks : kRopeFwdBlocks));
 #define BS_CALL(T, D, I) hipLaunchKernelGGL((rope_fwd_kernel<T, D, I, false>), grid, dim3(256), 0, stream, p)
   BS_ROPE_DISPATCH(BS_CALL);
 #undef BS_CALL
@@ -411,7 +466,8 @@ hipError_t launch_kv_append(const bs_dims& d, const bs_qk_params& P, const bs_pa
   p.num_seqs = num_seqs;
   p.max_pages = C.max_pages;
   p.page_shift = __builtin_ctz((unsigned)C.page_size);
-  const dim3 grid((unsigned)d.total_q);
+  p.together = together_of(d, kRows, (q.p != nullptr ? d.hq : 0) + d.hkv);
+  const dim3 grid((unsigned)((d.total_q + p.together - 1) / p.together));
 #define BS_CALL(T, D, I) hipLaunchKernelGGL((rope_fwd_kernel<T, D, I, true>), grid, dim3(256), 0, stream, p)
   BS_ROPE_DISPATCH(BS_CALL);
 #undef BS_CALL
@@ -431,7 +487,9 @@ hipError_t launch_qk_rope_bwd(const bs_dims& d, const bs_qk_params& P, Heads q, 
   p.dk = dk;
   const bool sums = dwq != nullptr || dwk != nullptr;
   p.part = sums ? part : nullptr;
-  const int blocks = (int)(d.total_q < kRopeBwdBlocks ? d.total_q : kRopeBwdBlocks);
+  p.together = together_of(d, 2, d.hq + d.hkv);
+  const int64_t need = (d.total_q + p.together - 1) / p.together;
+  const int blocks = (int)(need < kRopeBwdBlocks ? need : kRopeBwdBlocks);
   const dim3 grid((unsigned)blocks);
   if (blocks > 0) {
 #define BS_CALL(T, D, I) hipLaunchKernelGGL((rope_bwd_kernel<T, D, I>), grid, dim3(256), 0, stream, p)
@@ -439,7 +497,7 @@ hipError_t launch_qk_rope_bwd(const bs_dims& d, const bs_qk_params& P, Heads q, 
 #undef BS_CALL
   }
   if (sums)
-    hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)(2 * d.head_dim / 16)), dim3(256), 0, stream, part, blocks,
+    hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)(2 * d.head_dim / 16)), dim3(1024), 0, stream, part, blocks,
                        d.head_dim, dwq, dwk);
   return hipGetLastError();
 }
