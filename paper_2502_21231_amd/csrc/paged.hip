@@ -972,7 +972,8 @@ size_t paged_bytes(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k) {
 }
 
 bool paged_fits(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k, int64_t keys) {
-  if (!paged_layout(d, num_seqs, max_seqlen_k).line) return true;
+  const PagedLayout L = paged_layout(d, num_seqs, max_seqlen_k);
+  if (!L.line) return L.grid < (1 << 24);  // (a grid has less than 2^32 threads)
   const int64_t rows = d.total_q * (d.hq / d.hkv);
   const int64_t places = d.dtype == BS_BF16 ? (rows / kTileBM + num_seqs) * (keys / kTileBN + 3)
                                             : (rows / kFewBM + num_seqs) * (keys / 128 + 3);

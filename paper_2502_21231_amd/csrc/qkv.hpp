@@ -32,7 +32,7 @@ hipError_t launch_kv_append(const bs_dims& d, const bs_qk_params& P, const bs_pa
 
 constexpr int32_t kPagedMaxSeqs = 16384;
 size_t paged_bytes(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k);
-// Whether the call's blocks can be counted in 32 bits (keys: of a sequence at most).
+// Whether one launch holds the call and its blocks can be counted in 32 bits (keys: of a sequence at most).
 bool paged_fits(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k, int64_t keys);
 hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cache& C,
                             const int32_t* cu_q, int32_t num_seqs, int32_t max_seqlen_k, int causal,
