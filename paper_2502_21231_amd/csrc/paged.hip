@@ -63,7 +63,7 @@ struct PagedParams {
   PagedShare* share;  // [ranges], or [row blocks]
   float2* stat;       // [pieces][BM] (max in log2 units, sum)
   float* part;        // [pieces][BM][D]
-  int32_t parts;      // !kLine: workgroups of a row block at most
+  int32_t parts;      // items: workgroups of a row block at most
   int32_t bm;         // rows of a piece's room in stat and part
   int64_t total_q;
   int32_t num_seqs, max_pages, page_shift, max_len;
@@ -73,11 +73,14 @@ struct PagedParams {
 };
 
 constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32, kPagedGrid = 512;
-constexpr int kShortKeys = 1024;
+constexpr int kShortKeys = 1024, kFewWhole = 8;
 constexpr int kPartTiles = 4;  // key blocks of a part at least
 // Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
 // merge: 16 queries of 4 heads over 8K keys, 8 KV heads: 42 us from one block on, 31 from four).
 constexpr int kTileRange = 4;
+
+// How the work of a call is shared: a line, or items in the tile or in the few form.
+enum Mode { kLine = 0, kTileItems = 1, kFewItems = 2 };
 
 template <typename T, int D>
 constexpr int few_keys() { return sizeof(T) == 2 && D == 64 ? 64 : 32; }  // of a wave's tile
@@ -88,9 +91,9 @@ constexpr int few_keys() { return sizeof(T) == 2 && D == 64 ? 64 : 32; }  // of 
 struct Shape {
   int bm, blk;
 };
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __device__ __forceinline__ Shape shape_of(const PagedSeg& s) {
-  if (sizeof(T) == 4 || (kLine && (int64_t)s.lq * s.group <= kFewBM))
+  if (kMode == kFewItems || (kMode == kLine && (sizeof(T) == 4 || (int64_t)s.lq * s.group <= kFewBM)))
     return Shape{kFewBM, 4 * few_keys<T, D>()};
   return Shape{kTileBM, kTileBN};
 }
@@ -101,7 +104,7 @@ struct PagedLds {
   int32_t pre[257];  // places on the line before each thread's segments, per KV head
   int32_t sum[4];
   int32_t bad, tiles;
-  int32_t seg[256], q0[256], lq[256], lk[256];  // n = 1: the segment, its first query and lengths
+  __attribute__((aligned(16))) int32_t seg[256], q0[256], lq[256], lk[256];  // n = 1: the segment, its first query and lengths
 };
 
 __device__ __forceinline__ int32_t seqs_per_thread(int32_t n) { return (n + 255) >> 8; }
@@ -127,17 +130,17 @@ __device__ __forceinline__ int32_t wave_scan(int32_t x) {
 }
 
 // Places of a segment on the line, or its blocks of rows.
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __device__ __forceinline__ int32_t segment_cost(const PagedSeg& s) {
-  const Shape f = shape_of<T, D, kLine>(s);
-  if constexpr (!kLine) return paged_row_blocks(s, f.bm);
+  const Shape f = shape_of<T, D, kMode>(s);
+  if constexpr (kMode != kLine) return paged_row_blocks(s, f.bm);
   const PagedCost c = paged_cost(s, f.bm, f.blk);
   return c.start(c.n);
 }
 
 // Lays out the line (256 threads); the places per KV head, negative when the lengths are refused.  Block 0
 // writes the header.
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int32_t pt = seqs_per_thread(p.num_seqs);
@@ -165,8 +168,8 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
   int32_t sum = 0;
   bool tiles = false;
   auto count = [&](const PagedSeg& s) {
-    if (s.lq > 0) sum += segment_cost<T, D, kLine>(s);
-    tiles |= s.lq > 0 && shape_of<T, D, kLine>(s).bm == kTileBM;
+    if (s.lq > 0) sum += segment_cost<T, D, kMode>(s);
+    tiles |= s.lq > 0 && shape_of<T, D, kMode>(s).bm == kTileBM;
   };
   if (pt > 1) {
     for (int32_t b = tid * pt; b < min(tid * pt + pt, p.num_seqs); ++b) {
@@ -177,14 +180,20 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
     int32_t q0 = 0, at = tid;
     PagedSeg s = PagedSeg{0, -1, p.group, p.causal};
     if (tid < p.num_seqs) s = check(tid, q0);
-    if constexpr (!kLine) {
+    constexpr bool kRanked = kMode == kTileItems || (kMode == kFewItems && sizeof(T) == 4);
+    if constexpr (kRanked) {
       // the longest chains first, so that the last workgroups to start are short ones
       L.lk[tid] = s.lk;
       __syncthreads();
       at = 0;
-      for (int i = 0; i < p.num_seqs; ++i) {
-        const int32_t k = L.lk[i];
-        at += k > s.lk || (k == s.lk && i < tid);
+      const int4* all = reinterpret_cast<const int4*>(L.lk);
+#pragma unroll 4
+      for (int i = 0; i < p.num_seqs; i += 4) {  // (entries past num_seqs are -1)
+        const int4 k = all[i >> 2];
+        at += k.x > s.lk || (k.x == s.lk && i < tid);
+        at += k.y > s.lk || (k.y == s.lk && i + 1 < tid);
+        at += k.z > s.lk || (k.z == s.lk && i + 2 < tid);
+        at += k.w > s.lk || (k.w == s.lk && i + 3 < tid);
       }
       if (tid >= p.num_seqs) at = tid;
       __syncthreads();
@@ -193,7 +202,7 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
     L.q0[at] = q0;
     L.lq[at] = s.lq;
     L.lk[at] = s.lk;
-    if constexpr (!kLine) __syncthreads();
+    if constexpr (kRanked) __syncthreads();
     count(PagedSeg{L.lq[tid], L.lk[tid], p.group, p.causal});
   }
   const int32_t run = wave_scan(sum);
@@ -212,7 +221,7 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
   const int32_t bad = L.bad, all = __builtin_amdgcn_readfirstlane(L.pre[256]);
   if (blockIdx.x == 0 && tid == 0) {
     p.hdr->status = bad;
-    p.hdr->n_items = !kLine && bad == BS_DEV_OK ? all : 0;  // row blocks per KV head
+    p.hdr->n_items = kMode != kLine && bad == BS_DEV_OK ? all : 0;  // row blocks per KV head
   }
   return bad == BS_DEV_OK ? all : -1;
 }
@@ -221,7 +230,7 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
 struct Found {
   int32_t seg, q_start, lq, lk, before;
 };
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __device__ __forceinline__ Found find_segment(const PagedParams& p, const PagedLds& L, int32_t y) {
   const int lane = threadIdx.x & 63;
   int t = -1;
@@ -236,7 +245,7 @@ __device__ __forceinline__ Found find_segment(const PagedParams& p, const PagedL
     int32_t cost = 0;
     if (lane < pt && mine < p.num_seqs) {
       const PagedSeg s = paged_seg(p, mine);
-      if (s.lq > 0) cost = segment_cost<T, D, kLine>(s);
+      if (s.lq > 0) cost = segment_cost<T, D, kMode>(s);
     }
     const int32_t at = L.pre[t] + wave_scan(cost) - cost;
     const int k = __ffsll((unsigned long long)__ballot(cost > 0 && at <= y && y - at < cost)) - 1;
@@ -260,7 +269,7 @@ struct Piece {
   int32_t pieces;    // of the row block
 };
 
-// kLine: the piece that starts at place x (n <= 0: none); next: where the next row block starts.
+// Line: the piece that starts at place x (n <= 0: none); next: where the next row block starts.
 template <typename T, int D>
 __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds& L, int32_t line, int32_t per,
                                             int64_t x, int64_t x_end, int32_t range, Shape& f, int64_t& next) {
@@ -270,13 +279,13 @@ __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds
   if ((hk + 1) * (int64_t)line <= x) ++hk;
   c.hk = __builtin_amdgcn_readfirstlane(hk);
   const int32_t y = (int32_t)(x - c.hk * (int64_t)line);
-  const Found s = find_segment<T, D, true>(p, L, y);
+  const Found s = find_segment<T, D, kLine>(p, L, y);
   c.seg = s.seg;
   c.q_start = s.q_start;
   c.lq = s.lq;
   c.lk = s.lk;
   const PagedSeg g = PagedSeg{s.lq, s.lk, p.group, p.causal};
-  f = shape_of<T, D, true>(g);
+  f = shape_of<T, D, kLine>(g);
   const PagedCost k = paged_cost(g, f.bm, f.blk);
   c.rb = __builtin_amdgcn_readfirstlane(k.find(y - s.before));
   c.kb = __builtin_amdgcn_readfirstlane(y - s.before - k.start(c.rb));
@@ -294,20 +303,20 @@ __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds
 
 // The piece of workgroup b: a part of a row block, the row blocks of one segment and head side by side on one
 // XCD (b % 8), the longest first; line: row blocks per KV head.  false: none.
-template <typename T, int D>
+template <typename T, int D, int kMode>
 __device__ __forceinline__ bool item_piece(const PagedParams& p, const PagedLds& L, int32_t line, int32_t b,
                                            Piece& c) {
   const bool own = (p.hkv & 7) == 0;  // each XCD owns an eighth of the heads
   const int32_t hx = own ? p.hkv >> 3 : p.hkv, j = own ? b >> 3 : b;
   const int32_t i = j / (hx * p.parts);  // a row block's place, if all heads took turns
   if (i >= line) return false;
-  const Found g = find_segment<T, D, false>(p, L, i);
+  const Found g = find_segment<T, D, kMode>(p, L, i);
   c.seg = g.seg;
   c.q_start = g.q_start;
   c.lq = g.lq;
   c.lk = g.lk;
   const PagedSeg s = PagedSeg{g.lq, g.lk, p.group, p.causal};
-  const Shape f = shape_of<T, D, false>(s);
+  const Shape f = shape_of<T, D, kMode>(s);
   const int32_t nrb = paged_row_blocks(s, f.bm);
   const int32_t r = j - g.before * hx * p.parts;  // of the segment's nrb * hx * parts
   int32_t hl, u;  // head; row block and part
@@ -828,7 +837,7 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
   __syncthreads();  // the buffers are free
 }
 
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_kernel(const PagedParams p) {
   constexpr int N = buf_elems<T, D>();
@@ -838,23 +847,18 @@ void paged_kernel(const PagedParams p) {
   __shared__ FewLds F;
   __shared__ TileLds S;
 
-  const int32_t line = paged_line<T, D, kLine>(p, L);
+  const int32_t line = paged_line<T, D, kMode>(p, L);
   if (line < 0) return;
-  auto work = [&](const Piece& e, bool few) {
-    if constexpr (sizeof(T) == 4) {
-      few_piece<T, D, 0>(p, e, X, Y, F);
-    } else {
-      if (kLine && few) few_piece<T, D, 2>(p, e, X, Y, F);
-      else tile_piece<D>(p, e, X, Y, S);
-    }
-  };
-  if constexpr (!kLine) {
+  // non-temporal copies where a sequence's keys are read once
+  auto few = [&](const Piece& e) { few_piece<T, D, sizeof(T) == 2 ? 2 : 0>(p, e, X, Y, F); };
+  if constexpr (kMode != kLine) {
     Piece e;
-    if (!item_piece<T, D>(p, L, line, blockIdx.x, e)) return;
+    if (!item_piece<T, D, kMode>(p, L, line, blockIdx.x, e)) return;
     if (p.parts > 1 && e.kb == 0 && threadIdx.x == 0)
       p.share[e.at / p.parts] = PagedShare{e.pieces > 1 ? e.pieces : 0, e.at, e.at, 1, e.hk, e.rows,
-                                           e.rb * (sizeof(T) == 2 ? kTileBM : kFewBM), e.q_start};
-    work(e, false);
+                                           e.rb * (kMode == kFewItems ? kFewBM : kTileBM), e.q_start};
+    if constexpr (kMode == kFewItems) few(e);
+    else tile_piece<D>(p, e, X, Y, S);
   } else {
     PagedShare* share = p.share + blockIdx.x;
     const int64_t all = (int64_t)line * p.hkv;
@@ -876,7 +880,13 @@ void paged_kernel(const PagedParams p) {
           if (threadIdx.x == 0)
             *share = PagedShare{e.pieces, e.at, range * 2, 2, e.hk, e.rows, e.rb * f.bm, e.q_start};
         }
-        work(e, f.bm == kFewBM);
+        if constexpr (sizeof(T) == 2) {
+          if (f.bm != kFewBM) {
+            tile_piece<D>(p, e, X, Y, S);
+            continue;
+          }
+        }
+        few(e);
       }
     }
     if (!left_share && threadIdx.x == 0) share->pieces = 0;
@@ -884,13 +894,13 @@ void paged_kernel(const PagedParams p) {
 }
 
 // Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, D/4 lanes per
-// row.  kLine: by ranges, otherwise by row blocks.  Each lane weighs every D/4-th piece, so that no lane waits
+// row: by ranges of the line, or by row blocks.  Each lane weighs every D/4-th piece, so that no lane waits
 // for the pieces one after another.
-template <typename T, int D, bool kLine>
+template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
   constexpr int LPR = D / 4;
   if (p.hdr->status != BS_DEV_OK) return;
-  if (!kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;
+  if (kMode != kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;
   const PagedShare s = p.share[blockIdx.x];
   if (s.pieces == 0) return;
   const int ch = threadIdx.x % LPR, lane0 = threadIdx.x & 63 & ~(LPR - 1);
@@ -929,10 +939,10 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
 // What a call launches, from its shapes alone, and its workspace: header, shares, statistics and sums
 // of the pieces.
 struct PagedLayout {
-  bool line;
+  Mode mode;
   int32_t bm;      // rows of a piece's room
   int32_t grid;    // workgroups
-  int32_t parts;   // !line: of a row block
+  int32_t parts;   // items: of a row block
   int32_t shares;  // shares, and so workgroups in x of the merge (0: no merge)
   size_t share, stat, part, bytes;
 };
@@ -941,22 +951,30 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   L.share = L.stat = L.part = L.bytes = sizeof(WsHeader);
   const int64_t rows = d.total_q * (d.hq / d.hkv), seqs = num_seqs;
   const bool bf = d.dtype == BS_BF16;
-  // row blocks at most, if all are of the form that many rows take
-  const int64_t items = (rows / (bf ? kTileBM : kFewBM) + (rows < seqs ? rows : seqs)) * d.hkv;
-  // Few rows per sequence on average: the line.  Where all sequences are short, though, and their row blocks fill the
-  // chip, what a workgroup saves by an equal share is less than it takes to go from one piece to the next
-  // (64 sequences of up to 30 tokens over 500, 64/8 heads: line 61 us, items 35).
-  L.line = rows <= 2 * kTileBM * seqs && !(rows > kFewBM * seqs && items >= kPagedGrid && max_seqlen_k <= kShortKeys);
-  L.bm = bf && !(L.line && rows <= kFewBM) ? kTileBM : kFewBM;
+  auto blocks = [&](int bm) { return (rows / bm + (rows < seqs ? rows : seqs)) * d.hkv; };  // at most
+  const int few_block = 4 * (bf && d.head_dim == 64 ? 64 : 32);
+  // Few rows per sequence on average: the line.  Where all sequences are short, though, a row block's keys are not
+  // worth sharing, and what a workgroup saves by an equal share is less than the merge's launch, or than going from
+  // one piece to the next:
+  //   few rows, up to kFewWhole key blocks
+  //   more rows, up to kShortKeys keys, enough row blocks to fill the chip (64 sequences of up to 30 tokens over
+  //   500, 64/8 heads: line 61 us, items 35).
+  const Mode items = bf ? kTileItems : kFewItems;
+  if (seqs == 0) L.mode = kLine;
+  else if (rows <= kFewBM * seqs) L.mode = max_seqlen_k <= kFewWhole * few_block ? kFewItems : kLine;
+  else if (rows <= 2 * kTileBM * seqs) L.mode = blocks(bf ? kTileBM : kFewBM) >= kPagedGrid && max_seqlen_k <= kShortKeys ? items : kLine;
+  else L.mode = items;
+  L.bm = L.mode == kTileItems || (L.mode == kLine && bf && rows > kFewBM) ? kTileBM : kFewBM;
   int64_t pieces;
-  if (L.line) {
+  if (L.mode == kLine) {
     L.grid = L.shares = kPagedGrid;
     pieces = 2 * kPagedGrid;
   } else {
-    L.parts = items >= kPagedGrid ? 1 : (int32_t)(2 * kPagedGrid / items < 8 ? 2 * kPagedGrid / items : 8);
-    L.grid = (int32_t)(items * L.parts);
-    L.shares = L.parts > 1 ? (int32_t)items : 0;
-    pieces = L.parts > 1 ? items * L.parts : 0;
+    const int64_t n = blocks(L.bm);
+    L.parts = n >= kPagedGrid || rows <= kFewBM * seqs ? 1 : (int32_t)(2 * kPagedGrid / n < 8 ? 2 * kPagedGrid / n : 8);
+    L.grid = n > 0 ? (int32_t)(n * L.parts) : 1;  // (one workgroup checks the lengths)
+    L.shares = L.parts > 1 ? (int32_t)n : 0;
+    pieces = L.parts > 1 ? n * L.parts : 0;
   }
   if (L.shares == 0) return L;
   L.stat = L.share + align256(sizeof(PagedShare) * (size_t)L.shares);
@@ -973,7 +991,7 @@ size_t paged_bytes(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k) {
 
 bool paged_fits(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k, int64_t keys) {
   const PagedLayout L = paged_layout(d, num_seqs, max_seqlen_k);
-  if (!L.line) return L.grid < (1 << 24);  // (a grid has less than 2^32 threads)
+  if (L.mode != kLine) return L.grid < (1 << 24);  // (a grid has less than 2^32 threads)
   const int64_t rows = d.total_q * (d.hq / d.hkv);
   const int64_t places = d.dtype == BS_BF16 ? (rows / kTileBM + num_seqs) * (keys / kTileBN + 3)
                                             : (rows / kFewBM + num_seqs) * (keys / 128 + 3);
@@ -1017,18 +1035,19 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   p.group = d.hq / d.hkv;
   p.causal = causal;
   p.scale_log2 = scale * kLog2e;
-  if (W.grid == 0) return hipSuccess;
   // (4 or 16 workgroups share a block of rows in the merge)
   const dim3 grid((unsigned)W.grid), mgrid((unsigned)W.shares, W.bm == kFewBM ? 4 : 16);
-#define BS_LAUNCH(T, D, LINE)                                                               \
+#define BS_LAUNCH(T, D, MODE)                                                               \
   do {                                                                                      \
-    hipLaunchKernelGGL((paged_kernel<T, D, LINE>), grid, dim3(256), 0, stream, p);          \
+    hipLaunchKernelGGL((paged_kernel<T, D, MODE>), grid, dim3(256), 0, stream, p);          \
     if (W.shares > 0)                                                                       \
-      hipLaunchKernelGGL((paged_merge_kernel<T, D, LINE>), mgrid, dim3(256), 0, stream, p); \
+      hipLaunchKernelGGL((paged_merge_kernel<T, D, MODE>), mgrid, dim3(256), 0, stream, p); \
   } while (0)
-#define BS_CALL(T, D)                                               \
-  do {                                                              \
-    if (W.line) BS_LAUNCH(T, D, true); else BS_LAUNCH(T, D, false); \
+#define BS_CALL(T, D)                                                                                   \
+  do {                                                                                                  \
+    if (W.mode == kLine) BS_LAUNCH(T, D, kLine);                                                        \
+    else if (W.mode == kFewItems) BS_LAUNCH(T, D, kFewItems);                                           \
+    else if constexpr (sizeof(T) == 2) BS_LAUNCH(T, D, kTileItems);                                     \
   } while (0)
   if (d.dtype == BS_BF16) {
     if (d.head_dim == 128) BS_CALL(bf16, 128); else BS_CALL(bf16, 64);
