@@ -63,7 +63,7 @@ struct PagedParams {
   PagedShare* share;  // [ranges], or [row blocks]
   float2* stat;       // [pieces][BM] (max in log2 units, sum)
   float* part;        // [pieces][BM][D]
-  int32_t parts;      // items: workgroups of a row block at most
+  int32_t parts;      // items: whether row blocks may be shared (> 1)
   int32_t bm;         // rows of a piece's room in stat and part
   int64_t total_q;
   int32_t num_seqs, max_pages, page_shift, max_len;
@@ -72,7 +72,7 @@ struct PagedParams {
   float scale_log2;
 };
 
-constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32, kPagedGrid = 512;
+constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32, kPagedGrid = kPagedSlots;
 constexpr int kShortKeys = 1024, kFewWhole = 8;
 constexpr int kPartTiles = 4;  // key blocks of a part at least
 // Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
@@ -305,10 +305,10 @@ __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds
 // XCD (b % 8), the longest first; line: row blocks per KV head.  false: none.
 template <typename T, int D, int kMode>
 __device__ __forceinline__ bool item_piece(const PagedParams& p, const PagedLds& L, int32_t line, int32_t b,
-                                           Piece& c) {
+                                           int32_t max_parts, Piece& c) {
   const bool own = (p.hkv & 7) == 0;  // each XCD owns an eighth of the heads
   const int32_t hx = own ? p.hkv >> 3 : p.hkv, j = own ? b >> 3 : b;
-  const int32_t i = j / (hx * p.parts);  // a row block's place, if all heads took turns
+  const int32_t i = j / (hx * max_parts);  // a row block's place, if all heads took turns
   if (i >= line) return false;
   const Found g = find_segment<T, D, kMode>(p, L, i);
   c.seg = g.seg;
@@ -318,26 +318,26 @@ __device__ __forceinline__ bool item_piece(const PagedParams& p, const PagedLds&
   const PagedSeg s = PagedSeg{g.lq, g.lk, p.group, p.causal};
   const Shape f = shape_of<T, D, kMode>(s);
   const int32_t nrb = paged_row_blocks(s, f.bm);
-  const int32_t r = j - g.before * hx * p.parts;  // of the segment's nrb * hx * parts
+  const int32_t r = j - g.before * hx * max_parts;  // of the segment's nrb * hx * parts
   int32_t hl, u;  // head; row block and part
   if (own) {
-    hl = r / (nrb * p.parts);
-    u = r - hl * nrb * p.parts;
+    hl = r / (nrb * max_parts);
+    u = r - hl * nrb * max_parts;
   } else {
     u = r / hx;
     hl = r - u * hx;
   }
-  const int32_t back = u / p.parts, part = u - back * p.parts;
+  const int32_t back = u / max_parts, part = u - back * max_parts;
   c.hk = __builtin_amdgcn_readfirstlane(own ? (b & 7) * hx + hl : hl);
   c.rb = __builtin_amdgcn_readfirstlane(nrb - 1 - back);
   c.v = __builtin_amdgcn_readfirstlane(paged_blocks(s, f.bm, f.blk, c.rb));
   c.rows = min((int)(c.lq * p.group - c.rb * f.bm), f.bm);
-  c.pieces = min(p.parts, max(1, c.v / kPartTiles));
+  c.pieces = min(max_parts, max(1, c.v / kPartTiles));
   if (part >= c.pieces) return false;
   c.kb = __builtin_amdgcn_readfirstlane(part * c.v / c.pieces);
   c.n = __builtin_amdgcn_readfirstlane((part + 1) * c.v / c.pieces) - c.kb;
   // pieces and shares are numbered by head and row block
-  c.at = __builtin_amdgcn_readfirstlane((c.hk * line + g.before + c.rb) * p.parts + part);
+  c.at = __builtin_amdgcn_readfirstlane((c.hk * line + g.before + c.rb) * max_parts + part);
   return true;
 }
 
@@ -853,9 +853,18 @@ void paged_kernel(const PagedParams p) {
   auto few = [&](const Piece& e) { few_piece<T, D, sizeof(T) == 2 ? 2 : 0>(p, e, X, Y, F); };
   if constexpr (kMode != kLine) {
     Piece e;
-    if (!item_piece<T, D, kMode>(p, L, line, blockIdx.x, e)) return;
+    int32_t parts = 1;
+    if (p.parts > 1) {
+      // time of a key with its row block (a tile of 64 keys 2.1 us at head_dim 128; 128 keys in float32 4.5), and
+      // of a part's sums, written and read at 4 TB/s
+      constexpr float us = (sizeof(T) == 2 ? 0.033f : 0.035f) * (D == 128 ? 1.f : 0.55f);
+      constexpr float piece = (sizeof(T) == 2 ? kTileBM : kFewBM) * D * 2e-6f;
+      const int32_t keys = p.num_seqs <= 256 ? L.lk[0] : p.max_len;  // (the longest comes first)
+      parts = __builtin_amdgcn_readfirstlane(paged_parts(line * p.hkv, (float)keys * us, piece));
+    }
+    if (!item_piece<T, D, kMode>(p, L, line, blockIdx.x, parts, e)) return;
     if (p.parts > 1 && e.kb == 0 && threadIdx.x == 0)
-      p.share[e.at / p.parts] = PagedShare{e.pieces > 1 ? e.pieces : 0, e.at, e.at, 1, e.hk, e.rows,
+      p.share[e.at / parts] = PagedShare{e.pieces > 1 ? e.pieces : 0, e.at, e.at, 1, e.hk, e.rows,
                                            e.rb * (kMode == kFewItems ? kFewBM : kTileBM), e.q_start};
     if constexpr (kMode == kFewItems) few(e);
     else tile_piece<D>(p, e, X, Y, S);
@@ -942,7 +951,7 @@ struct PagedLayout {
   Mode mode;
   int32_t bm;      // rows of a piece's room
   int32_t grid;    // workgroups
-  int32_t parts;   // items: of a row block
+  int32_t parts;   // items: of a row block at most
   int32_t shares;  // shares, and so workgroups in x of the merge (0: no merge)
   size_t share, stat, part, bytes;
 };
@@ -971,10 +980,11 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
     pieces = 2 * kPagedGrid;
   } else {
     const int64_t n = blocks(L.bm);
-    L.parts = n >= kPagedGrid || rows <= kFewBM * seqs ? 1 : (int32_t)(2 * kPagedGrid / n < 8 ? 2 * kPagedGrid / n : 8);
-    L.grid = n > 0 ? (int32_t)(n * L.parts) : 1;  // (one workgroup checks the lengths)
+    L.parts = n >= kPagedSlots || rows <= kFewBM * seqs ? 1 : kPagedMaxParts;
+    pieces = n * L.parts < 2 * kPagedSlots ? n * L.parts : 2 * kPagedSlots;  // (what paged_parts keeps to)
+    L.grid = L.parts == 1 ? (int32_t)(n > 0 ? n : 1) : (int32_t)pieces;      // (one workgroup checks the lengths)
     L.shares = L.parts > 1 ? (int32_t)n : 0;
-    pieces = L.parts > 1 ? n * L.parts : 0;
+    if (L.shares == 0) pieces = 0;
   }
   if (L.shares == 0) return L;
   L.stat = L.share + align256(sizeof(PagedShare) * (size_t)L.shares);

@@ -97,6 +97,30 @@ BS_HD PagedRanges paged_ranges(int64_t all, int32_t grid, int32_t least) {
 BS_HD int32_t paged_pieces(int32_t at, int32_t v, int32_t per) {
   return (int32_t)(((uint32_t)at + (uint32_t)v - 1) / (uint32_t)per) + 1;
 }
+// Workgroups that run at a time (two per CU), and parts of a row block's keys at most.
+constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 8;
+// Into how many parts the keys of n < kPagedSlots row blocks are cut, n times that at most 2 kPagedSlots: the
+// smallest estimate, in microseconds, of
+//   chain x rounds of workgroups / parts  +  5 for the merge's launch and `piece` for each part's sums,
+// the rounds between the whole number that equal chains take and what uneven ones, the longest first, take on
+// average.  chain: time of the longest.  Measured, us: one sequence of 512 new tokens over 14K, 64/8 heads (256 row
+// blocks): 2 parts 166, 4 parts 177; 700 over 9K, 48/8 (264): 1 part 160, 3 parts 134; 900 over 1K, 64/8 (450): 1
+// part 65, 2 parts 83; 128 over 16K, 64/8 (64): 4 parts 57, 8 parts 55.
+BS_HD int32_t paged_parts(int32_t n, float chain, float piece) {
+  int32_t best = 1;
+  float least = 1e30f;
+  for (int32_t p = 1; p <= kPagedMaxParts && (p == 1 || n * p <= 2 * kPagedSlots); ++p) {
+    const float x = (float)(n * p) / kPagedSlots + 0.4f, even = x > 1.f ? x : 1.f;
+    const float whole = (float)((n * p + kPagedSlots - 1) / kPagedSlots);
+    const float cost = chain * (0.7f * whole + 0.3f * even) / (float)p + (p > 1 ? 5.f + piece * (float)(n * p) : 0.f);
+    if (cost < least) {
+      least = cost;
+      best = p;
+    }
+  }
+  return best;
+}
+
 // Range of block b of the grid: blocks are dealt to the 8 XCDs in turn, and each XCD takes neighbouring
 // ranges, which read the same keys.  -1: none.
 BS_HD int32_t paged_range_of(int32_t b, int32_t active) {

@@ -116,5 +116,11 @@ int main() {
       CHECK(R.per >= 1 && R.active * (int64_t)R.per >= R.all && (R.active == 0 || (R.active - 1) * (int64_t)R.per < R.all));
       CHECK(R.active <= 512 && (R.per == 1 || (R.per - 1) * (int64_t)512 < R.all));
     }
+  for (int32_t n = 0; n < kPagedSlots; ++n) {
+    for (float chain : {0.f, 2.f, 100.f, 1e6f}) {
+      const int32_t parts = paged_parts(n, chain, 0.033f);
+      CHECK(parts >= 1 && parts <= kPagedMaxParts && n * parts <= 2 * kPagedSlots);
+    }
+  }
   std::puts("ok");
 }
