@@ -70,14 +70,19 @@ def _call(t, fn, *args) -> None:
         B._check(fn(*args, B._stream(t)))
 
 
-def _heads(t, name, dtype=None) -> int:
-    """Checks a [T, heads, d] tensor on the GPU whose heads are contiguous; elements from token to token."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and (dtype is None or t.dtype is dtype):
-        T, h, d = t.shape
-        s = t.stride()
-        if (s[2] == 1 or d == 1) and (s[1] == d or h == 1):
-            return s[0] if T > 1 else h * d
-        raise ValueError(f"{name}: the heads of a token must be contiguous (strides {s})")
+# Small calls are bound by this module's own time: the checks pass their common case with few attribute reads.
+
+
+def _heads(t, name, dtype=None):
+    """Checks a [T, heads, d] tensor on the GPU whose heads are contiguous; (elements from token to token, shape)."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and (dtype is None or t.dtype is dtype):
+        shape = t.shape
+        if len(shape) == 3:
+            T, h, d = shape
+            s0, s1, s2 = t.stride()
+            if (s2 == 1 or d == 1) and (s1 == d or h == 1):
+                return (s0 if T > 1 else h * d), shape
+            raise ValueError(f"{name}: the heads of a token must be contiguous (strides {t.stride()})")
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -85,10 +90,6 @@ def _heads(t, name, dtype=None) -> int:
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
     raise ValueError(f"{name} must have 3 dimensions (got {t.dim()})")
-
-
-def _dims(q_shape, hq, hkv, dtype) -> B.bs_dims:
-    return B.bs_dims(q_shape[0], 0, hq, hkv, q_shape[2], dtype)
 
 
 def _same_device(device, **tensors):
@@ -103,11 +104,12 @@ class QkParams:
     def __init__(self, struct, tensors, head_dim, device):
         self.struct, self.tensors, self.head_dim, self.device = struct, tensors, head_dim, device
         self.ref = ctypes.byref(struct)
+        self.index = None if device is None else device.index
 
-    def check(self, t):
-        if self.head_dim is not None and t.shape[2] != self.head_dim:
-            raise ValueError(f"the weights have {self.head_dim} elements, a head {t.shape[2]}")
-        if self.device is not None and t.device != self.device:
+    def check(self, t, d):
+        if self.head_dim != d and self.head_dim is not None:
+            raise ValueError(f"the weights have {self.head_dim} elements, a head {d}")
+        if self.index != t.get_device() and self.index is not None:
             raise ValueError(f"params are on {self.device}, the tokens on {t.device}")
 
 
@@ -142,16 +144,16 @@ class PagedCache:
         self.struct, self.k, self.v, self.block_table, self.kv_lens = struct, k, v, block_table, kv_lens
         self.ref = ctypes.byref(struct)
         self.hkv, self.head_dim, self.dtype = k.shape[2], k.shape[3], k.dtype
-        self.num_seqs, self.device = kv_lens.numel(), k.device
+        self.num_seqs, self.device, self.index = kv_lens.numel(), k.device, k.device.index
 
-    def check(self, t, cu_seqlens_q) -> int:
+    def check(self, t, d, cu_seqlens_q) -> int:
         """The number of sequences, for tokens t [T, heads, d]."""
-        if t.dtype is not self.dtype or t.shape[2] != self.head_dim or t.device != self.device:
+        if t.dtype is not self.dtype or d != self.head_dim or t.get_device() != self.index:
             raise ValueError(f"the cache holds {self.dtype} heads of {self.head_dim} elements on {self.device}")
         B._need(cu_seqlens_q, "cu_seqlens_q", torch.int32, 1)
-        n = cu_seqlens_q.numel() - 1
-        if n != self.num_seqs or cu_seqlens_q.device != self.device:
-            raise ValueError(f"cu_seqlens_q must have {self.num_seqs + 1} entries on {self.device}")
+        n = self.num_seqs
+        if cu_seqlens_q.numel() != n + 1 or cu_seqlens_q.get_device() != self.index:
+            raise ValueError(f"cu_seqlens_q must have {n + 1} entries on {self.device}")
         return n
 
 
@@ -190,12 +192,17 @@ def make_paged_cache(k, v, block_table, kv_lens) -> PagedCache:
     return PagedCache(s, k, v, block_table, kv_lens)
 
 
-def _qk(q, k, params):
-    qs, ks = _heads(q, "q"), _heads(k, "k", q.dtype)
-    if q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+def _qk(q, k, positions, params):
+    """Strides of q and k, and the sizes (T, hq, hkv, d)."""
+    qs, (T, hq, d) = _heads(q, "q")
+    ks, (Tk, hkv, dk) = _heads(k, "k", q.dtype)
+    if T != Tk or d != dk:
         raise ValueError(f"shape mismatch q {tuple(q.shape)} k {tuple(k.shape)}")
-    params.check(q)
-    return qs, ks
+    params.check(q, d)
+    B._need(positions, "positions", torch.int64, 1)
+    if positions.shape[0] != T:
+        raise ValueError("one position per token")
+    return qs, ks, T, hq, hkv, d
 
 
 def _out(t, like, name):
@@ -208,22 +215,16 @@ def _out(t, like, name):
     return t
 
 
-def _positions(positions, q):
-    B._need(positions, "positions", torch.int64, 1)
-    if positions.numel() != q.shape[0]:
-        raise ValueError("one position per token")
-
-
 def bs_qk_norm_rope_fwd(q, k, positions, params: QkParams, q_out=None, k_out=None):
     """Norm and rotation of q [T, hq, d] and k [T, hkv, d] (contiguous heads, any stride from token to
     token: parts of a fused projection's output will do) at `positions` (int64 [T]).  Returns contiguous
     (q_out, k_out) for the attention; they may be q and k themselves."""
-    qs, ks = _qk(q, k, params)
-    _positions(positions, q)
+    qs, ks, T, hq, hkv, d = _qk(q, k, positions, params)
     q_out, k_out = _out(q_out, q, "q_out"), _out(k_out, k, "k_out")
-    dims = _dims(q.shape, q.shape[1], k.shape[1], B._dtype_code(q))
-    _call(q, _library().bs_qk_norm_rope_fwd, ctypes.byref(dims), params.ref, B._ptr(q), qs, B._ptr(k), ks,
-          B._ptr(positions), B._ptr(q_out), B._ptr(k_out))
+    dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(q))
+    p = B._ptr
+    _call(q, _library().bs_qk_norm_rope_fwd, ctypes.byref(dims), params.ref, p(q), qs, p(k), ks, p(positions),
+          p(q_out), p(k_out))
     return q_out, k_out
 
 
@@ -236,8 +237,21 @@ def bs_qk_norm_rope_workspace_size(dims: B.bs_dims) -> int:
 
 def alloc_qk_workspace(q, k) -> torch.Tensor:
     """Workspace of bs_qk_norm_rope_bwd for tokens like these."""
-    dims = _dims(q.shape, q.shape[1], k.shape[1], B._dtype_code(q))
+    dims = B.bs_dims(q.shape[0], 0, q.shape[1], k.shape[1], q.shape[2], B._dtype_code(q))
     return torch.empty(bs_qk_norm_rope_workspace_size(dims), dtype=torch.uint8, device=q.device)
+
+
+def _dweight(given, w, name, d, device):
+    if w is None:
+        if given is not None:
+            raise ValueError(f"{name}: the gradient of a weight that the params do not have")
+        return None
+    if given is None:
+        return torch.empty(d, dtype=torch.float32, device=device)
+    B._need(given, name, torch.float32, 1)
+    if given.shape[0] != d:
+        raise ValueError(f"{name} must have {d} elements")
+    return given
 
 
 def bs_qk_norm_rope_bwd(q, k, positions, params: QkParams, dq_out, dk_out, dq=None, dk=None, dq_weight=None,
@@ -245,38 +259,28 @@ def bs_qk_norm_rope_bwd(q, k, positions, params: QkParams, dq_out, dk_out, dq=No
     """Gradients of bs_qk_norm_rope_fwd's inputs from those of its outputs (contiguous).  q, k: the forward's
     inputs.  dq, dk may be strided like q and k (parts of the projection's gradient), or dq_out and dk_out
     themselves.  Returns (dq, dk, dq_weight, dk_weight); the weights' are float32 [d], None without weights."""
-    qs, ks = _qk(q, k, params)
-    _positions(positions, q)
-    B._need(dq_out, "dq_out", q.dtype, 3)
-    B._need(dk_out, "dk_out", q.dtype, 3)
-    if dq_out.shape != q.shape or dk_out.shape != k.shape:
-        raise ValueError("dq_out and dk_out must have the shapes of q and k")
+    qs, ks, T, hq, hkv, d = _qk(q, k, positions, params)
+    dt = q.dtype
+    B._need(dq_out, "dq_out", dt, 3)
+    B._need(dk_out, "dk_out", dt, 3)
     if dq is None:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dq = torch.empty((T, hq, d), dtype=dt, device=q.device)
     if dk is None:
-        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dqs, dks = _heads(dq, "dq", q.dtype), _heads(dk, "dk", k.dtype)
-    if dq.shape != q.shape or dk.shape != k.shape:
-        raise ValueError("dq and dk must have the shapes of q and k")
+        dk = torch.empty((T, hkv, d), dtype=dt, device=q.device)
+    dqs, q_shape = _heads(dq, "dq", dt)
+    dks, k_shape = _heads(dk, "dk", dt)
+    if q_shape != (T, hq, d) or k_shape != (T, hkv, d) or dq_out.shape != q_shape or dk_out.shape != k_shape:
+        raise ValueError("dq_out, dk_out, dq and dk must have the shapes of q and k")
     _, wq, wk = params.tensors
-    d = q.shape[2]
-    if wq is None and dq_weight is not None or wk is None and dk_weight is not None:
-        raise ValueError("the gradient of a weight that the params do not have")
-    if wq is not None and dq_weight is None:
-        dq_weight = torch.empty(d, dtype=torch.float32, device=q.device)
-    if wk is not None and dk_weight is None:
-        dk_weight = torch.empty(d, dtype=torch.float32, device=q.device)
-    for w, name in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
-        if w is not None:
-            B._need(w, name, torch.float32, 1)
-            if w.numel() != d:
-                raise ValueError(f"{name} must have {d} elements")
+    dq_weight = _dweight(dq_weight, wq, "dq_weight", d, params.device)
+    dk_weight = _dweight(dk_weight, wk, "dk_weight", d, params.device)
     if workspace is None and (wq is not None or wk is not None):
         workspace = alloc_qk_workspace(q, k)
-    dims = _dims(q.shape, q.shape[1], k.shape[1], B._dtype_code(q))
-    _call(q, _library().bs_qk_norm_rope_bwd, ctypes.byref(dims), params.ref, B._ptr(q), qs, B._ptr(k), ks,
-          B._ptr(positions), B._ptr(dq_out), B._ptr(dk_out), B._ptr(dq), dqs, B._ptr(dk), dks, B._ptr(dq_weight),
-          B._ptr(dk_weight), B._ptr(workspace), 0 if workspace is None else workspace.numel())
+    dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(q))
+    p = B._ptr
+    _call(q, _library().bs_qk_norm_rope_bwd, ctypes.byref(dims), params.ref, p(q), qs, p(k), ks, p(positions),
+          p(dq_out), p(dk_out), p(dq), dqs, p(dk), dks, p(dq_weight), p(dk_weight), p(workspace),
+          0 if workspace is None else workspace.numel())
     return dq, dk, dq_weight, dk_weight
 
 
@@ -285,23 +289,27 @@ def bs_kv_append(q, k, v, cache: PagedCache, cu_seqlens_q, params: QkParams | No
     [T, hkv, d] are the last tokens of sequence b, whose cache.kv_lens[b] counts them already.  Keys go
     through `params` at their position; so do the queries q [T, hq, d] (or None), into q_out, which is
     returned.  Rows behind the last sequence are left alone (an own q_out then holds whatever its memory did)."""
-    ks, vs = _heads(k, "k"), _heads(v, "v", k.dtype)
-    if k.shape != v.shape or k.shape[1] != cache.hkv:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} must have the cache's {cache.hkv} heads")
-    nseq = cache.check(k, cu_seqlens_q)
+    ks, k_shape = _heads(k, "k")
+    vs, v_shape = _heads(v, "v", k.dtype)
+    T, hkv, d = k_shape
+    if k_shape != v_shape or hkv != cache.hkv:
+        raise ValueError(f"k {tuple(k_shape)} and v {tuple(v_shape)} must have the cache's {cache.hkv} heads")
+    nseq = cache.check(k, d, cu_seqlens_q)
     if params is not None:
-        params.check(k)
-    qs, hq = 0, cache.hkv
+        params.check(k, d)
+    qs, hq = 0, hkv
     if q is not None:
-        qs, hq = _heads(q, "q", k.dtype), q.shape[1]
-        if q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2] or q.device != k.device:
-            raise ValueError(f"shape mismatch q {tuple(q.shape)} k {tuple(k.shape)}")
+        qs, (Tq, hq, dq) = _heads(q, "q", k.dtype)
+        if Tq != T or dq != d or q.get_device() != cache.index:
+            raise ValueError(f"shape mismatch q {tuple(q.shape)} k {tuple(k_shape)}")
         q_out = _out(q_out, q, "q_out")
-    dims = _dims(k.shape, hq, cache.hkv, B._dtype_code(k))
+    else:
+        q_out = None
+    dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(k))
+    p = B._ptr
     _call(k, _library().bs_kv_append, ctypes.byref(dims), None if params is None else params.ref, cache.ref,
-          B._ptr(cu_seqlens_q), nseq, B._ptr(q), qs, B._ptr(k), ks, B._ptr(v), vs,
-          B._ptr(q_out) if q is not None else None)
-    return q_out if q is not None else None
+          p(cu_seqlens_q), nseq, p(q), qs, p(k), ks, p(v), vs, p(q_out))
+    return q_out
 
 
 def bs_attn_paged_workspace_size(dims: B.bs_dims, num_seqs: int, max_seqlen_k: int) -> int:
@@ -313,7 +321,7 @@ def bs_attn_paged_workspace_size(dims: B.bs_dims, num_seqs: int, max_seqlen_k: i
 
 def alloc_paged_workspace(q, cache: PagedCache, max_seqlen_k: int) -> torch.Tensor:
     """Workspace of bs_attn_paged_fwd for queries like these over this cache."""
-    dims = _dims(q.shape, q.shape[1], cache.hkv, B._dtype_code(q))
+    dims = B.bs_dims(q.shape[0], 0, q.shape[1], cache.hkv, q.shape[2], B._dtype_code(q))
     return torch.empty(bs_attn_paged_workspace_size(dims, cache.num_seqs, int(max_seqlen_k)), dtype=torch.uint8,
                        device=q.device)
 
@@ -324,8 +332,8 @@ def bs_attn_paged_fwd(q, cache: PagedCache, cu_seqlens_q, max_seqlen_k: int, cau
     iff j <= i + kv_len - n, with causal).  Returns (out [T, hq, d], lse float32 [hq, T]); rows behind the last
     sequence are left as they were."""
     B._need(q, "q", None, 3)
-    nseq = cache.check(q, cu_seqlens_q)
     T, hq, d = q.shape
+    nseq = cache.check(q, d, cu_seqlens_q)
     out = _out(out, q, "out")
     if lse is None:
         lse = torch.empty(hq, T, dtype=torch.float32, device=q.device)
@@ -335,8 +343,8 @@ def bs_attn_paged_fwd(q, cache: PagedCache, cu_seqlens_q, max_seqlen_k: int, cau
             raise ValueError(f"lse must have the shape {(hq, T)}")
     if workspace is None:
         workspace = alloc_paged_workspace(q, cache, max_seqlen_k)
-    dims = _dims(q.shape, hq, cache.hkv, B._dtype_code(q))
-    _call(q, _library().bs_attn_paged_fwd, ctypes.byref(dims), B._ptr(q), cache.ref, B._ptr(cu_seqlens_q), nseq,
-          int(max_seqlen_k), int(bool(causal)), B._scale(scale, d), B._ptr(out), B._ptr(lse), B._ptr(workspace),
-          workspace.numel())
+    dims = B.bs_dims(T, 0, hq, cache.hkv, d, B._dtype_code(q))
+    p = B._ptr
+    _call(q, _library().bs_attn_paged_fwd, ctypes.byref(dims), p(q), cache.ref, p(cu_seqlens_q), nseq,
+          int(max_seqlen_k), int(bool(causal)), B._scale(scale, d), p(out), p(lse), p(workspace), workspace.numel())
     return out, lse
