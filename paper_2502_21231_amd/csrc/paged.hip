@@ -72,7 +72,7 @@ struct PagedParams {
   float scale_log2;
 };
 
-constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32, kPagedGrid = kPagedSlots;
+constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32;
 constexpr int kShortKeys = 1024, kFewWhole = 8;
 constexpr int kPartTiles = 4;  // key blocks of a part at least
 // Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
@@ -271,13 +271,11 @@ struct Piece {
 
 // Line: the piece that starts at place x (n <= 0: none); next: where the next row block starts.
 template <typename T, int D>
-__device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds& L, int32_t line, int32_t per,
-                                            int64_t x, int64_t x_end, int32_t range, Shape& f, int64_t& next) {
+__device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds& L, int32_t line,
+                                            const PagedRanges& R, int64_t x, int64_t x_end, int32_t range, Shape& f,
+                                            int64_t& next) {
   Piece c;
-  int32_t hk = (int32_t)((double)x / line);
-  if (hk * (int64_t)line > x) --hk;
-  if ((hk + 1) * (int64_t)line <= x) ++hk;
-  c.hk = __builtin_amdgcn_readfirstlane(hk);
+  c.hk = __builtin_amdgcn_readfirstlane(paged_head(x, line));
   const int32_t y = (int32_t)(x - c.hk * (int64_t)line);
   const Found s = find_segment<T, D, kLine>(p, L, y);
   c.seg = s.seg;
@@ -286,15 +284,22 @@ __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds
   c.lk = s.lk;
   const PagedSeg g = PagedSeg{s.lq, s.lk, p.group, p.causal};
   f = shape_of<T, D, kLine>(g);
-  const PagedCost k = paged_cost(g, f.bm, f.blk);
-  c.rb = __builtin_amdgcn_readfirstlane(k.find(y - s.before));
-  c.kb = __builtin_amdgcn_readfirstlane(y - s.before - k.start(c.rb));
-  next = x + __builtin_amdgcn_readfirstlane(s.before + k.start(c.rb + 1) - y);
-  c.v = __builtin_amdgcn_readfirstlane(paged_blocks(g, f.bm, f.blk, c.rb));
+  if (s.lq * p.group <= f.bm) {  // one row block: its places are its blocks
+    c.rb = 0;
+    c.kb = y - s.before;
+    c.v = paged_blocks(g, f.bm, f.blk, 0);
+    next = x + c.v - c.kb;
+  } else {
+    const PagedCost k = paged_cost(g, f.bm, f.blk);
+    c.rb = __builtin_amdgcn_readfirstlane(k.find(y - s.before));
+    c.kb = __builtin_amdgcn_readfirstlane(y - s.before - k.start(c.rb));
+    next = x + __builtin_amdgcn_readfirstlane(s.before + k.start(c.rb + 1) - y);
+    c.v = __builtin_amdgcn_readfirstlane(paged_blocks(g, f.bm, f.blk, c.rb));
+  }
   c.n = (int32_t)min((int64_t)(c.v - c.kb), x_end - x);
   c.rows = min((int)(c.lq * p.group - c.rb * f.bm), f.bm);
   // (the number of pieces is wanted where the row block starts only)
-  c.pieces = c.n == c.v ? 1 : c.kb > 0 ? 2 : paged_pieces((int32_t)(x - (int64_t)range * per), c.v, per);
+  c.pieces = c.n == c.v ? 1 : c.kb > 0 ? 2 : __builtin_amdgcn_readfirstlane(R.of(x + c.v - 1)) - range + 1;
   // a range has at most one piece that goes on from the range before (place 0 of its two) and one that
   // another range goes on with (place 1)
   c.at = range * 2 + (c.kb == 0);
@@ -848,7 +853,10 @@ void paged_kernel(const PagedParams p) {
   __shared__ TileLds S;
 
   const int32_t line = paged_line<T, D, kMode>(p, L);
-  if (line < 0) return;
+  if (line < 0) {  // nothing is written
+    if (kMode == kLine && threadIdx.x == 0) p.share[blockIdx.x].pieces = 0;
+    return;
+  }
   // non-temporal copies where a sequence's keys are read once
   auto few = [&](const Piece& e) { few_piece<T, D, sizeof(T) == 2 ? 2 : 0>(p, e, X, Y, F); };
   if constexpr (kMode != kLine) {
@@ -870,18 +878,16 @@ void paged_kernel(const PagedParams p) {
     else tile_piece<D>(p, e, X, Y, S);
   } else {
     PagedShare* share = p.share + blockIdx.x;
-    const int64_t all = (int64_t)line * p.hkv;
-    const PagedRanges R = paged_ranges(all, gridDim.x, L.tiles ? kTileRange : 1);
-    const int32_t per = __builtin_amdgcn_readfirstlane(R.per);
-    const int32_t range = paged_range_of(blockIdx.x, __builtin_amdgcn_readfirstlane(R.active));
+    const PagedRanges R((int64_t)line * p.hkv, __builtin_amdgcn_readfirstlane(L.tiles) ? kTileRange : 1);
+    const int32_t range = paged_range_of(blockIdx.x, R.n);
     bool left_share = false;
     if (range >= 0) {
-      int64_t x = (int64_t)range * per;
-      const int64_t x_end = min(all, x + per);
+      int64_t x = R.start(range);
+      const int64_t x_end = R.start(range + 1);
       while (x < x_end) {
         Shape f;
         int64_t next;
-        const Piece e = line_piece<T, D>(p, L, line, per, x, x_end, range, f, next);
+        const Piece e = line_piece<T, D>(p, L, line, R, x, x_end, range, f, next);
         x = e.kb + e.n >= e.v || e.n <= 0 ? next : x_end;
         if (e.n <= 0) continue;
         if (e.pieces > 1 && e.kb == 0) {
@@ -908,8 +914,7 @@ void paged_kernel(const PagedParams p) {
 template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
   constexpr int LPR = D / 4;
-  if (p.hdr->status != BS_DEV_OK) return;
-  if (kMode != kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;
+  if (kMode != kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;  // (0 items if lengths are refused)
   const PagedShare s = p.share[blockIdx.x];
   if (s.pieces == 0) return;
   const int ch = threadIdx.x % LPR, lane0 = threadIdx.x & 63 & ~(LPR - 1);
@@ -971,13 +976,13 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   const Mode items = bf ? kTileItems : kFewItems;
   if (seqs == 0) L.mode = kLine;
   else if (rows <= kFewBM * seqs) L.mode = max_seqlen_k <= kFewWhole * few_block ? kFewItems : kLine;
-  else if (rows <= 2 * kTileBM * seqs) L.mode = blocks(bf ? kTileBM : kFewBM) >= kPagedGrid && max_seqlen_k <= kShortKeys ? items : kLine;
+  else if (rows <= 2 * kTileBM * seqs) L.mode = blocks(bf ? kTileBM : kFewBM) >= kPagedSlots && max_seqlen_k <= kShortKeys ? items : kLine;
   else L.mode = items;
   L.bm = L.mode == kTileItems || (L.mode == kLine && bf && rows > kFewBM) ? kTileBM : kFewBM;
   int64_t pieces;
   if (L.mode == kLine) {
-    L.grid = L.shares = kPagedGrid;
-    pieces = 2 * kPagedGrid;
+    L.grid = L.shares = kPagedSlots;
+    pieces = 2 * kPagedSlots;
   } else {
     const int64_t n = blocks(L.bm);
     L.parts = n >= kPagedSlots || rows <= kFewBM * seqs ? 1 : kPagedMaxParts;

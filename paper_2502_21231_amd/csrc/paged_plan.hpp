@@ -74,31 +74,41 @@ BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
   return c;
 }
 
-// Workgroups' ranges of a line of `all` places: `per` each (at least `least`), `active` of them not empty.  A line
-// has less than 2^31 places per KV head and less than 2^31 times the grid in all: the entry point refuses more.
+// Workgroups that run at a time (two per CU), the ranges of a line at most, and parts of a row block's keys at most.
+constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 8;
+
+// The n <= kPagedSlots ranges of a line of `all` places, of `least` or more places each (one range: all), as equal as
+// can be.  A line has less than 2^31 places per KV head and less than 2^39 in all: the entry point refuses more.
 struct PagedRanges {
   int64_t all;
-  int32_t per, active;
+  int32_t n;
+  BS_HD PagedRanges(int64_t places, int32_t least) : all(places) {
+    n = kPagedSlots;
+    if (all < (int64_t)kPagedSlots * least) {
+      n = (int32_t)all / least;
+      if (n < 1) n = all > 0 ? 1 : 0;
+    }
+  }
+  BS_HD int64_t start(int32_t w) const {
+    if (n == kPagedSlots) return w * all / kPagedSlots;  // (a shift)
+    return n > 0 ? (uint32_t)w * (uint32_t)all / (uint32_t)n : 0;
+  }
+  // The range that place x lies in (a float quotient is off by one at most).
+  BS_HD int32_t of(int64_t x) const {
+    int32_t w = (int32_t)((float)(x + 1) * (float)n / (float)all);
+    if (w > n - 1) w = n - 1;
+    while (start(w) > x) --w;
+    while (start(w + 1) <= x) ++w;
+    return w;
+  }
 };
-BS_HD PagedRanges paged_ranges(int64_t all, int32_t grid, int32_t least) {
-  PagedRanges r;
-  r.all = all;
-  // (a quotient in float64 is off by one at most here)
-  int64_t per = (int64_t)((double)(all + grid - 1) / (double)grid);
-  if (per * grid < all) ++per;
-  if (per < least) per = least;
-  r.per = (int32_t)per;
-  r.active = (int32_t)((double)(all + per - 1) / (double)per);
-  while ((int64_t)r.active * per < all) ++r.active;
-  while (r.active > 0 && (int64_t)(r.active - 1) * per >= all) --r.active;
-  return r;
+// Floor of x / line, below 2^12.
+BS_HD int32_t paged_head(int64_t x, int32_t line) {
+  int32_t h = (int32_t)((float)x / (float)line);
+  while (h * (int64_t)line > x) --h;
+  while ((h + 1) * (int64_t)line <= x) ++h;
+  return h;
 }
-// Ranges that share a row block of v places whose first lies `at` places into its range.
-BS_HD int32_t paged_pieces(int32_t at, int32_t v, int32_t per) {
-  return (int32_t)(((uint32_t)at + (uint32_t)v - 1) / (uint32_t)per) + 1;
-}
-// Workgroups that run at a time (two per CU), and parts of a row block's keys at most.
-constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 8;
 // Into how many parts the keys of n < kPagedSlots row blocks are cut, n times that at most 2 kPagedSlots: the
 // smallest estimate, in microseconds, of
 //   chain x rounds of workgroups / parts  +  5 for the merge's launch and `piece` for each part's sums,
@@ -121,11 +131,11 @@ BS_HD int32_t paged_parts(int32_t n, float chain, float piece) {
   return best;
 }
 
-// Range of block b of the grid: blocks are dealt to the 8 XCDs in turn, and each XCD takes neighbouring
+// Range, of n, of block b of the grid: blocks are dealt to the 8 XCDs in turn, and each XCD takes neighbouring
 // ranges, which read the same keys.  -1: none.
-BS_HD int32_t paged_range_of(int32_t b, int32_t active) {
-  const int32_t each = (active + 7) >> 3, at = b >> 3, w = (b & 7) * each + at;
-  return at < each && w < active ? w : -1;
+BS_HD int32_t paged_range_of(int32_t b, int32_t n) {
+  const int32_t each = (n + 7) >> 3, at = b >> 3, w = (b & 7) * each + at;
+  return at < each && w < n ? w : -1;
 }
 
 }  // namespace bs

@@ -42,8 +42,17 @@ static void segment(const PagedSeg& s, int BM, int BLK) {
   if (c.n == 1) CHECK(c.start(1) == need);
 }
 
+static void ranges(const PagedRanges& R, int least) {
+  CHECK(R.n <= kPagedSlots && (R.n > 0) == (R.all > 0) && R.start(0) == 0 && (R.n == 0 || R.start(R.n) == R.all));
+  for (int32_t w = 0; w < R.n; ++w) {
+    const int64_t a = R.start(w), b = R.start(w + 1);
+    CHECK(b > a && (b - a >= least || R.n == 1) && b - a <= R.all / R.n + 1);
+    CHECK(R.of(a) == w && R.of(b - 1) == w);
+  }
+}
+
 // Segments of up to 32 rows take the first shape, others the second.
-static void line(const std::vector<PagedSeg>& segs, int hkv, int grid, int least) {
+static void line(const std::vector<PagedSeg>& segs, int hkv, int least) {
   const int bm[2] = {32, 128}, blk[2] = {128, 64};
   auto kind = [&](const PagedSeg& s) { return (int64_t)s.lq * s.group <= 32 ? 0 : 1; };
   int64_t per_head = 0;
@@ -53,29 +62,30 @@ static void line(const std::vector<PagedSeg>& segs, int hkv, int grid, int least
     const int t = kind(s);
     if (s.lq > 0) per_head += paged_cost(s, bm[t], blk[t]).start(paged_row_blocks(s, bm[t]));
   }
-  const PagedRanges R = paged_ranges(per_head * hkv, grid, least);
-  CHECK(R.active <= grid && R.active * (int64_t)R.per >= R.all && (R.active == 0 || (R.active - 1) * (int64_t)R.per < R.all));
-  std::vector<int> taken(grid, 0);
-  for (int32_t b = 0; b < grid; ++b) {
-    const int32_t w = paged_range_of(b, R.active);
-    CHECK(w >= -1 && w < R.active);
+  const PagedRanges R(per_head * hkv, least);
+  ranges(R, least);
+  std::vector<int> taken(kPagedSlots, 0);
+  for (int32_t b = 0; b < kPagedSlots; ++b) {
+    const int32_t w = paged_range_of(b, R.n);
+    CHECK(w >= -1 && w < R.n);
     if (w >= 0) CHECK(++taken[w] == 1);
   }
-  for (int32_t w = 0; w < R.active; ++w) CHECK(taken[w] == 1);
-  std::vector<int> heads_of(R.active, 0), tails_of(R.active, 0);  // pieces that leave sums: one of each at most
+  for (int32_t w = 0; w < R.n; ++w) CHECK(taken[w] == 1);
+  std::vector<int> heads_of(R.n, 0), tails_of(R.n, 0);  // pieces that leave sums: one of each at most
   for (int h = 0; h < hkv; ++h)
     for (size_t b = 0; b < segs.size(); ++b) {
       if (segs[b].lq == 0) continue;
       const int t = kind(segs[b]);
       const PagedCost c = paged_cost(segs[b], bm[t], blk[t]);
       for (int32_t i = 0; i < c.n; ++i) {
-        const int64_t xs = h * per_head + pre[b] + c.start(i), first = xs / R.per;
-        const int32_t v = paged_blocks(segs[b], bm[t], blk[t], i);
-        const int32_t pieces = paged_pieces((int32_t)(xs - first * R.per), v, R.per);
+        const int64_t xs = h * per_head + pre[b] + c.start(i);
+        CHECK(c.n > 1 || c.start(1) == paged_blocks(segs[b], bm[t], blk[t], 0));
+        const int32_t v = paged_blocks(segs[b], bm[t], blk[t], i), first = R.of(xs), pieces = R.of(xs + v - 1) - first + 1;
         int64_t done = 0;
         for (int32_t k = 0; k < pieces; ++k) {
-          const int64_t w = first + k, lo = std::max(w * R.per, xs), hi = std::min((w + 1) * R.per, xs + v);
-          CHECK(w < R.active && lo - xs == done && hi > lo);
+          const int32_t w = first + k;
+          const int64_t lo = std::max(R.start(w), xs), hi = std::min(R.start(w + 1), xs + v);
+          CHECK(w < R.n && lo - xs == done && hi > lo);
           done += hi - lo;
           if (pieces > 1) CHECK(++(lo == xs ? heads_of : tails_of)[w] == 1);
         }
@@ -108,14 +118,18 @@ int main() {
     std::vector<PagedSeg> segs(rng() % 20);
     const int32_t group = pick(1, 16), causal = rng() % 4 != 0;
     for (PagedSeg& s : segs) s = PagedSeg{(int32_t)(rng() % 5 ? pick(1, 300) : 0), pick(1, 3000) - 1, group, causal};
-    line(segs, 1 + rng() % 9, n % 2 ? 512 : 8 * (1 + rng() % 64), 1 + n % 5);
+    line(segs, 1 + rng() % 9, 1 + n % 5);
   }
   for (int64_t all : {(int64_t)0, (int64_t)1, (int64_t)511, (int64_t)512, (int64_t)513, ((int64_t)1 << 39) - 1})
     for (int n = 0; n < 2000; ++n) {
-      const PagedRanges R = paged_ranges(all - n * (all >> 12), 512, 1);
-      CHECK(R.per >= 1 && R.active * (int64_t)R.per >= R.all && (R.active == 0 || (R.active - 1) * (int64_t)R.per < R.all));
-      CHECK(R.active <= 512 && (R.per == 1 || (R.per - 1) * (int64_t)512 < R.all));
+      const PagedRanges R(all - n * (all >> 12), 1 + n % 5);
+      ranges(R, 1 + n % 5);
     }
+  for (int n = 0; n < 300000; ++n) {
+    const int32_t len = pick(1, (1 << 30)), h = rng() % 4096;
+    const int64_t x = h * (int64_t)len + rng() % len;
+    CHECK(paged_head(x, len) == h && paged_head(h * (int64_t)len, len) == h && paged_head((h + 1) * (int64_t)len - 1, len) == h);
+  }
   for (int32_t n = 0; n < kPagedSlots; ++n) {
     for (float chain : {0.f, 2.f, 100.f, 1e6f}) {
       const int32_t parts = paged_parts(n, chain, 0.033f);
