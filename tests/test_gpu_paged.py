@@ -91,32 +91,61 @@ CASES = [
 ]
 
 
-@pytest.mark.parametrize("case", CASES, ids=str)
+# more of them, where the work is shared otherwise: keys of several workgroups, prompts of many rows, both forms in
+# one call, row blocks in parts
+SHARED = [
+    ([3000, 10, 700], [1, 1, 1], 16, 8, 2, 128, BF),
+    ([2900, 2500], [1, 4], 64, 12, 2, 64, BF),
+    ([1500, 2100, 40, 9], [1, 150, 1, 1], 16, 12, 4, 128, BF),
+    ([600, 1300, 70], [3, 200, 1], 16, 8, 1, 64, BF),
+    ([1200, 900], [500, 900], 32, 4, 2, 128, BF),
+    ([700], [700], 16, 1, 1, 64, BF),
+    ([2000], [40], 16, 32, 1, 128, BF),
+    ([1700, 30], [1, 1], 16, 8, 2, 128, F32),
+    ([900, 300], [300, 280], 16, 4, 4, 64, F32),
+    ([500, 600], [400, 1], 32, 6, 2, 128, F32),
+]
+
+
+@pytest.mark.parametrize("case", CASES + SHARED, ids=str)
 @pytest.mark.parametrize("hm", [False, True])
 def test_against_oracle(gpu, case, hm):
     run_case(*case, hm=hm, seed=len(case[0]))
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_loose_bound(gpu, case):
+    """A max_seqlen_k far above the lengths (a context's, say), which chooses another way to share the work."""
+    run_case(*case, seed=1, most=1 << 20)
+
+
+def test_not_causal(gpu):
+    for case in (CASES[1], CASES[5], CASES[10], SHARED[2], SHARED[4], SHARED[8]):
+        run_case(*case, seed=2, causal=False)
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("causal", [True, False])
 def test_rows_without_keys_and_padding(gpu, dt, causal):
     """Sequences without keys, with more rows than keys (the first see none), without rows; padding rows."""
-    run_case([0, 5, 300, 0, 80], [1, 9, 0, 0, 200], 16, 8, 2, 128, dt, pad=7, causal=causal)
+    for most in (300, 5000):
+        run_case([0, 5, 300, 0, 80], [1, 9, 0, 0, 200], 16, 8, 2, 128, dt, pad=7, causal=causal, most=most)
     run_case([0, 0], [3, 1], 16, 4, 4, 64, dt, pad=1, causal=causal)
     run_case([300, 64], [1, 70], 32, 4, 1, 64, dt, causal=causal, most=100000 // 3)
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
-@pytest.mark.parametrize("new", [1, 40])
-def test_missing_pages(gpu, dt, new):
+@pytest.mark.parametrize("new", [1, 40, 100])
+@pytest.mark.parametrize("most", [330, 5000])
+def test_missing_pages(gpu, dt, new, most):
     """Pages that are not there hide their keys: first, middle, last ones, all of a sequence's."""
     def edit(kc, vc, table):
         n = kc.shape[0]
         table[0, [0, 5, 6, 7, 8, 20]] = [-1, n, -2 ** 31, 2 ** 31 - 1, -1, n + 5]
         table[1, :] = -1
         table[2, 1:] = -9
-    run_case([330, 100, 100], [new] * 3, 16, 8, 2, 128, dt, edit=edit)
-    run_case([330, 100, 100], [new] * 3, 16, 4, 4, 64, dt, edit=edit, hm=True, causal=False)
+    run_case([330, 100, 100], [new] * 3, 16, 8, 2, 128, dt, edit=edit, most=most)
+    run_case([330, 100, 100], [new] * 3, 16, 4, 4, 64, dt, edit=edit, hm=True, causal=False, most=most)
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
@@ -158,8 +187,14 @@ def test_many_sequences(gpu):
     rng = np.random.default_rng(0)
     lens = [int(x) for x in rng.integers(0, 40, 1500)]
     new = [int(min(n, x)) for n, x in zip(lens, rng.integers(0, 3, 1500))]
-    run_case(lens, new, 16, 2, 1, 64, BF)
-    run_case(lens[:700], new[:700], 16, 2, 2, 64, F32)
+    for most in (40, 5000):
+        run_case(lens, new, 16, 2, 1, 64, BF, most=most)
+        run_case(lens[:700], new[:700], 16, 2, 2, 64, F32, most=most)
+    lens = [int(x) for x in rng.integers(30, 200, 300)]
+    new = [int(min(n, x)) for n, x in zip(lens, rng.integers(0, 60, 300))]
+    run_case(lens, new, 16, 16, 1, 64, BF)  # 480 rows on average
+    run_case(lens, new, 16, 16, 1, 64, F32)
+    run_case(lens[:260], new[:260], 16, 8, 1, 64, BF, most=3000)
 
 
 def test_refused_lengths_write_nothing(gpu):
@@ -233,11 +268,11 @@ def test_two_streams_and_repeats(gpu):
         assert torch.equal(a, c) and torch.equal(b, d)
 
 
-@pytest.mark.parametrize("hq,hkv,T", [(16, 2, 4), (8, 8, 90)])
-def test_captured_step_replayed_with_other_lengths(gpu, hq, hkv, T):
+@pytest.mark.parametrize("hq,hkv,T,most", [(16, 2, 4, 600), (16, 2, 4, 2000), (8, 8, 90, 600), (8, 2, 90, 4000), (8, 1, 400, 600)])
+def test_captured_step_replayed_with_other_lengths(gpu, hq, hkv, T, most):
     """One captured step of a padded batch (append, attention), replayed as the sequences grow and as their
     number of rows changes, against eager calls; a second capture shares the workspace."""
-    d, page, nseq, most = 64, 16, 4, 600
+    d, page = 64, 16
     kc, vc = (torch.zeros(200, page, hkv, d, dtype=BF, device=gpu) for _ in range(2))
     table = torch.arange(4 * 40, dtype=torch.int32, device=gpu).view(4, 40)
     lens, cu = torch.zeros(4, dtype=torch.int32, device=gpu), torch.zeros(5, dtype=torch.int32, device=gpu)
@@ -265,7 +300,7 @@ def test_captured_step_replayed_with_other_lengths(gpu, hq, hkv, T):
     rng = np.random.default_rng(0)
     have = np.zeros(4, int)
     for i in range(6):
-        new = np.array([1, 1, 1, 1]) if T == 4 else np.array([1, 50 if i % 2 else 0, rng.integers(1, 30), 1])
+        new = np.array([1, 1, 1, 1]) if T == 4 else np.array([1, T // 2 if i % 2 and i < 4 else 0, rng.integers(1, 30), 1])
         if i == 3:
             new[1] = 0  # a sequence leaves: its rows and its length
         have = have + new + (100 if i == 2 else 0)

@@ -47,6 +47,10 @@ CASES = [
     (2500, 2, 2, 64, torch.float32, torch.bfloat16, 48, False, 7),
     (3, 40, 8, 128, torch.bfloat16, "k", 112, False, 500),
     (1, 512, 8, 64, torch.bfloat16, torch.float32, 64, True, 1 << 20),
+    # several tokens per workgroup, the last one short of them; outputs that are larger than the caches
+    (8195, 2, 1, 64, torch.bfloat16, torch.bfloat16, 64, False, 0),
+    (4101, 3, 1, 128, torch.float32, torch.float32, 128, True, 3),
+    (14001, 8, 2, 128, torch.bfloat16, torch.float32, 96, False, 5),
 ]
 
 
@@ -214,6 +218,7 @@ APPENDS = [
     ([40, 17, 5], [23, 17, 0], 16, 8, 8, 64, torch.float32, True, 64, True, True, 3),
     ([0, 300, 2], [1, 290, 3], 64, 4, 2, 128, torch.bfloat16, False, 64, False, True, 2),
     ([4096], [77], 256, 7, 7, 64, torch.bfloat16, False, 0, False, False, 0),
+    ([5000, 3201], [4999, 3197], 64, 2, 1, 64, torch.bfloat16, True, 64, False, False, 3),
 ]
 
 
