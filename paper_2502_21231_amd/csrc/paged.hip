@@ -548,6 +548,19 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
     wait_vmem_all();
     __syncthreads();
   };
+  if (w * 32 >= e.rows) {  // a wave without rows copies its keys, and leaves the matrix core to the others
+    for (int t = t0; t < n_tiles; ++t) {
+      if (t + 1 < n_tiles) {
+        const int odd = (t + 1 - t0) & 1;
+        bf16* Z = odd ? Y : X;
+        copy(t + 1, page, Z, Z + TILE, S.miss[odd]);
+        page = page_of(t + 2);
+      }
+      wait_vmem_all();
+      __syncthreads();
+    }
+    return;
+  }
   int t = t0;
   for (; t + 2 < n_tiles; t += 2) {
     step(std::true_type{}, t, X, X + TILE, S.miss[0], Y, Y + TILE, S.miss[1]);
