@@ -98,6 +98,13 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} is on {t.device}, not on {device}")
 
 
+def _one_device(index, *tensors):
+    """Refuses tensors (or None) that are not on the GPU `index`; a workspace in host memory is one."""
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"a tensor is on {t.device}, the tokens are on cuda:{index}")
+
+
 class QkParams:
     """Rotation and norm of queries and keys (see `make_qk_params`)."""
 
@@ -221,6 +228,7 @@ def bs_qk_norm_rope_fwd(q, k, positions, params: QkParams, q_out=None, k_out=Non
     (q_out, k_out) for the attention; they may be q and k themselves."""
     qs, ks, T, hq, hkv, d = _qk(q, k, positions, params)
     q_out, k_out = _out(q_out, q, "q_out"), _out(k_out, k, "k_out")
+    _one_device(q.get_device(), k, positions, q_out, k_out)
     dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(q))
     p = B._ptr
     _call(q, _library().bs_qk_norm_rope_fwd, ctypes.byref(dims), params.ref, p(q), qs, p(k), ks, p(positions),
@@ -276,6 +284,7 @@ def bs_qk_norm_rope_bwd(q, k, positions, params: QkParams, dq_out, dk_out, dq=No
     dk_weight = _dweight(dk_weight, wk, "dk_weight", d, params.device)
     if workspace is None and (wq is not None or wk is not None):
         workspace = alloc_qk_workspace(q, k)
+    _one_device(q.get_device(), k, positions, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace)
     dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(q))
     p = B._ptr
     _call(q, _library().bs_qk_norm_rope_bwd, ctypes.byref(dims), params.ref, p(q), qs, p(k), ks, p(positions),
@@ -300,11 +309,12 @@ def bs_kv_append(q, k, v, cache: PagedCache, cu_seqlens_q, params: QkParams | No
     qs, hq = 0, hkv
     if q is not None:
         qs, (Tq, hq, dq) = _heads(q, "q", k.dtype)
-        if Tq != T or dq != d or q.get_device() != cache.index:
+        if Tq != T or dq != d:
             raise ValueError(f"shape mismatch q {tuple(q.shape)} k {tuple(k_shape)}")
         q_out = _out(q_out, q, "q_out")
     else:
         q_out = None
+    _one_device(cache.index, q, v, q_out)
     dims = B.bs_dims(T, 0, hq, hkv, d, B._dtype_code(k))
     p = B._ptr
     _call(k, _library().bs_kv_append, ctypes.byref(dims), None if params is None else params.ref, cache.ref,
@@ -343,6 +353,7 @@ def bs_attn_paged_fwd(q, cache: PagedCache, cu_seqlens_q, max_seqlen_k: int, cau
             raise ValueError(f"lse must have the shape {(hq, T)}")
     if workspace is None:
         workspace = alloc_paged_workspace(q, cache, max_seqlen_k)
+    _one_device(cache.index, out, lse, workspace)
     dims = B.bs_dims(T, 0, hq, cache.hkv, d, B._dtype_code(q))
     p = B._ptr
     _call(q, _library().bs_attn_paged_fwd, ctypes.byref(dims), p(q), cache.ref, p(cu_seqlens_q), nseq,

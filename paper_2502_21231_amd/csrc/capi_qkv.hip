@@ -286,6 +286,10 @@ int bs_attn_paged_fwd(const bs_dims* dims, const void* q, const bs_paged_cache* 
     return fail(BS_ERR_WORKSPACE, "workspace is not 256-byte aligned");
   if (workspace_bytes < need)
     return fail(BS_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
+  const int64_t lb = d.total_q * d.hq * 4;
+  if (overlaps(lse, lb, q, bytes) || overlaps(lse, lb, out, bytes) || overlaps(lse, lb, cache->k, cb) ||
+      overlaps(lse, lb, cache->v, cb))
+    return fail(BS_ERR_INVALID_ARG, "lse overlaps another operand");
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope ps(BS_KERNEL_PAGED, s);
   BS_HIP(launch_paged_fwd(d, q, *cache, cu_seqlens_q, num_seqs, max_seqlen_k, causal, scale, out, lse, workspace, s),

@@ -243,6 +243,8 @@ def test_refused_arguments(gpu):
         Q.bs_attn_paged_fwd(q, cache, cu, 40, scale=-1.0)
     with pytest.raises(B.BsError):
         Q.bs_attn_paged_fwd(q, cache, cu, 40, workspace=torch.empty(16, dtype=torch.uint8, device=gpu))
+    with pytest.raises(ValueError, match="is on cpu"):
+        Q.bs_attn_paged_fwd(q, cache, cu, 40, workspace=torch.empty(1 << 24, dtype=torch.uint8))
 
 
 def test_two_streams_and_repeats(gpu):

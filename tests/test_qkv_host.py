@@ -183,3 +183,20 @@ def test_binding_refuses_tensors_on_the_host():
         Q.make_paged_cache(pages, pages, torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
     with pytest.raises(ValueError, match="page_size"):
         Q.make_paged_cache(x, x, None, None)
+
+
+def test_lse_overlaps_nothing(lib):
+    for at in (Q_AT + 64, QO_AT, FAKE + 256, FAKE + (1 << 30)):
+        said(BAD, paged(lib, lse=at, ws=KO_AT), "lse overlaps another operand")
+
+
+def test_binding_refuses_tensors_elsewhere():
+    class On:
+        def __init__(self, index):
+            self.device = "cpu" if index < 0 else f"cuda:{index}"
+            self.get_device = lambda: index
+
+    Q._one_device(1, On(1), None, On(1))
+    for index in (-1, 0):
+        with pytest.raises(ValueError, match=On(index).device):
+            Q._one_device(1, On(1), On(index))
