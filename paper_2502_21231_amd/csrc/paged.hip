@@ -74,7 +74,6 @@ struct PagedParams {
 
 constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32;
 constexpr int kShortKeys = 1024, kFewWhole = 8;
-constexpr int kPartTiles = 4;  // key blocks of a part at least
 // Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
 // merge: 16 queries of 4 heads over 8K keys, 8 KV heads: 42 us from one block on, 31 from four).
 constexpr int kTileRange = 4;
@@ -337,7 +336,7 @@ __device__ __forceinline__ bool item_piece(const PagedParams& p, const PagedLds&
   c.rb = __builtin_amdgcn_readfirstlane(nrb - 1 - back);
   c.v = __builtin_amdgcn_readfirstlane(paged_blocks(s, f.bm, f.blk, c.rb));
   c.rows = min((int)(c.lq * p.group - c.rb * f.bm), f.bm);
-  c.pieces = min(max_parts, max(1, c.v / kPartTiles));
+  c.pieces = min(max_parts, c.v);  // (up to 4 blocks in a part at least: 3 x 200 over 700, float32, 31 us instead of 21)
   if (part >= c.pieces) return false;
   c.kb = __builtin_amdgcn_readfirstlane(part * c.v / c.pieces);
   c.n = __builtin_amdgcn_readfirstlane((part + 1) * c.v / c.pieces) - c.kb;
