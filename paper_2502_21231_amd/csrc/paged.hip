@@ -5,17 +5,17 @@
 // one.  A workgroup of four waves takes one of two forms for a block of rows:
 //   few   32 rows; the waves take 32 (bf16, head_dim 64: 64) keys in turn, each with LDS buffers, page
 //         numbers and a softmax of its own, joined at the end: bound by reading the keys, no barrier
-//         between copies (the layout of few_bf16.hip).  All float32 calls take it, on the float32
-//         matrix instruction;
+//         between copies (the layout of few_bf16.hip).  Sequences of up to 32 rows, and all float32
+//         ones, on the float32 matrix instruction;
 //   tile  bf16, 128 rows over tiles of 64 keys that the waves share, 32 rows each: bound by the matrix
 //         core (the layout of fwd_bf16.hip).
-// How the work is shared:
-//   line  the blocks of all sequences form one line cut into equal ranges (paged_plan.hpp); a sequence
-//         of up to 32 rows is worked off in the few form and others in the tile form, side by side, so
-//         that a step of decoding and prompt chunks uses memory and matrix core at once;
-//   items where sequences have many rows: a workgroup per block of rows, or per part of its keys when
-//         there are too few; those of a sequence and head run next to one another on one XCD and
-//         walk the same keys in step, which then come into its L2 once.
+// Both side by side in one launch, so that a step of decoding and prompt chunks uses memory and matrix
+// core at once.  How the work is shared:
+//   line  the blocks of all sequences form one line cut into equal ranges (paged_plan.hpp): decoding,
+//         where row blocks are few and their lengths differ;
+//   items where sequences have many rows, or few keys: a workgroup per block of rows, or per part of its
+//         keys when there are too few; those of a sequence and head run next to one another on one XCD
+//         and walk the same keys in step, which then come into its L2 once.
 // A block of rows that several workgroups share leaves (O, max, sum) of each part in float32, and
 // paged_merge_kernel combines them.  Every workgroup lays out the line from the lengths itself: only
 // shapes are known on the host, so a captured call can be replayed with other lengths.
@@ -92,7 +92,7 @@ struct Shape {
 };
 template <typename T, int D, int kMode>
 __device__ __forceinline__ Shape shape_of(const PagedSeg& s) {
-  if (kMode == kFewItems || (kMode == kLine && (sizeof(T) == 4 || (int64_t)s.lq * s.group <= kFewBM)))
+  if (kMode == kFewItems || sizeof(T) == 4 || (int64_t)s.lq * s.group <= kFewBM)
     return Shape{kFewBM, 4 * few_keys<T, D>()};
   return Shape{kTileBM, kTileBN};
 }
@@ -303,6 +303,17 @@ __device__ __forceinline__ Piece line_piece(const PagedParams& p, const PagedLds
   // another range goes on with (place 1)
   c.at = range * 2 + (c.kb == 0);
   return c;
+}
+
+// paged_parts, one number of parts per lane (one after another they take 5 us).
+__device__ __forceinline__ int32_t best_parts(int32_t n, float chain, float piece) {
+  static_assert(kPagedMaxParts <= 64, "a lane for each");
+  const int32_t lane = threadIdx.x & 63;
+  const float mine = lane < kPagedMaxParts ? paged_part_cost(n, lane + 1, chain, piece) : 1e30f;
+  float least = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) least = fminf(least, __shfl_xor(least, off));
+  return __ffsll((unsigned long long)__ballot(mine == least));
 }
 
 // The piece of workgroup b: a part of a row block, the row blocks of one segment and head side by side on one
@@ -880,14 +891,17 @@ void paged_kernel(const PagedParams p) {
       constexpr float us = (sizeof(T) == 2 ? 0.033f : 0.035f) * (D == 128 ? 1.f : 0.55f);
       constexpr float piece = (sizeof(T) == 2 ? kTileBM : kFewBM) * D * 2e-6f;
       const int32_t keys = p.num_seqs <= 256 ? L.lk[0] : p.max_len;  // (the longest comes first)
-      parts = __builtin_amdgcn_readfirstlane(paged_parts(line * p.hkv, (float)keys * us, piece));
+      parts = __builtin_amdgcn_readfirstlane(best_parts(line * p.hkv, (float)keys * us, piece));
     }
     if (!item_piece<T, D, kMode>(p, L, line, blockIdx.x, parts, e)) return;
     if (p.parts > 1 && e.kb == 0 && threadIdx.x == 0)
       p.share[e.at / parts] = PagedShare{e.pieces > 1 ? e.pieces : 0, e.at, e.at, 1, e.hk, e.rows,
                                            e.rb * (kMode == kFewItems ? kFewBM : kTileBM), e.q_start};
-    if constexpr (kMode == kFewItems) few(e);
-    else tile_piece<D>(p, e, X, Y, S);
+    if (kMode == kFewItems || e.lq * p.group <= kFewBM) {
+      few(e);
+    } else {
+      if constexpr (kMode != kFewItems) tile_piece<D>(p, e, X, Y, S);
+    }
   } else {
     PagedShare* share = p.share + blockIdx.x;
     const PagedRanges R((int64_t)line * p.hkv, __builtin_amdgcn_readfirstlane(L.tiles) ? kTileRange : 1);
@@ -979,17 +993,16 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   const bool bf = d.dtype == BS_BF16;
   auto blocks = [&](int bm) { return (rows / bm + (rows < seqs ? rows : seqs)) * d.hkv; };  // at most
   const int few_block = 4 * (bf && d.head_dim == 64 ? 64 : 32);
-  // Few rows per sequence on average: the line.  Where all sequences are short, though, a row block's keys are not
-  // worth sharing, and what a workgroup saves by an equal share is less than the merge's launch, or than going from
-  // one piece to the next:
-  //   few rows, up to kFewWhole key blocks
-  //   more rows, up to kShortKeys keys, enough row blocks to fill the chip (64 sequences of up to 30 tokens over
-  //   500, 64/8 heads: line 61 us, items 35).
-  const Mode items = bf ? kTileItems : kFewItems;
+  // Up to 32 rows per sequence on average: the line, unless all sequences are so short (kFewWhole key blocks) that
+  // what a workgroup saves by an equal share is less than the merge's launch.  More rows: items (measured, us, line /
+  // items: a chunk of 500 and 32 single queries over 8K, 64/8 heads 167 / 151; of 900 and 64 over 4K, 32/8 148 / 113;
+  // 8 x 30 over 4K, 64/8 44 / 38; but 32 x 30 over 8K 164 / 207, where chains are uneven).  In float32 up to 256 rows
+  // per sequence take the line where there are fewer row blocks than workgroups (a chunk of 300 and 32 single queries
+  // over 4K, 32/4, head_dim 64: 72 / 104) or keys are many.
+  L.mode = bf ? kTileItems : kFewItems;
   if (seqs == 0) L.mode = kLine;
   else if (rows <= kFewBM * seqs) L.mode = max_seqlen_k <= kFewWhole * few_block ? kFewItems : kLine;
-  else if (rows <= 2 * kTileBM * seqs) L.mode = blocks(bf ? kTileBM : kFewBM) >= kPagedSlots && max_seqlen_k <= kShortKeys ? items : kLine;
-  else L.mode = items;
+  else if (!bf && rows <= 2 * kTileBM * seqs && (blocks(kFewBM) < kPagedSlots || max_seqlen_k > kShortKeys)) L.mode = kLine;
   L.bm = L.mode == kTileItems || (L.mode == kLine && bf && rows > kFewBM) ? kTileBM : kFewBM;
   int64_t pieces;
   if (L.mode == kLine) {

@@ -75,7 +75,7 @@ BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
 }
 
 // Workgroups that run at a time (two per CU), the ranges of a line at most, and parts of a row block's keys at most.
-constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 8;
+constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 64;
 
 // The n <= kPagedSlots ranges of a line of `all` places, of `least` or more places each (one range: all), as equal as
 // can be.  A line has less than 2^31 places per KV head and less than 2^39 in all: the entry point refuses more.
@@ -111,23 +111,22 @@ BS_HD int32_t paged_head(int64_t x, int32_t line) {
 }
 // Into how many parts the keys of n < kPagedSlots row blocks are cut, n times that at most 2 kPagedSlots: the
 // smallest estimate, in microseconds, of
-//   chain x rounds of workgroups / parts  +  5 for the merge's launch and `piece` for each part's sums,
+//   chain x rounds of workgroups / parts  +  5 for the merge's launch, 0.2 for each of a row block's parts, which it
+//   reads one after another, and `piece` for each part's sums,
 // the rounds between the whole number that equal chains take and what uneven ones, the longest first, take on
 // average.  chain: time of the longest.  Measured, us: one sequence of 512 new tokens over 14K, 64/8 heads (256 row
 // blocks): 2 parts 166, 4 parts 177; 700 over 9K, 48/8 (264): 1 part 160, 3 parts 134; 900 over 1K, 64/8 (450): 1
-// part 65, 2 parts 83; 128 over 16K, 64/8 (64): 4 parts 57, 8 parts 55.
+// part 65, 2 parts 83; 128 over 16K, 64/8 (64): 4 parts 57, 8 parts 55; 300 over 60K, 8/2 (20): 8 parts 86, 45 63.
+BS_HD float paged_part_cost(int32_t n, int32_t p, float chain, float piece) {
+  if (p > 1 && n * p > 2 * kPagedSlots) return 1e30f;
+  const float x = (float)(n * p) / kPagedSlots + 0.4f, even = x > 1.f ? x : 1.f;
+  const float whole = (float)((n * p + kPagedSlots - 1) / kPagedSlots);
+  return chain * (0.7f * whole + 0.3f * even) / (float)p + (p > 1 ? 5.f + 0.2f * (float)p + piece * (float)(n * p) : 0.f);
+}
 BS_HD int32_t paged_parts(int32_t n, float chain, float piece) {
   int32_t best = 1;
-  float least = 1e30f;
-  for (int32_t p = 1; p <= kPagedMaxParts && (p == 1 || n * p <= 2 * kPagedSlots); ++p) {
-    const float x = (float)(n * p) / kPagedSlots + 0.4f, even = x > 1.f ? x : 1.f;
-    const float whole = (float)((n * p + kPagedSlots - 1) / kPagedSlots);
-    const float cost = chain * (0.7f * whole + 0.3f * even) / (float)p + (p > 1 ? 5.f + piece * (float)(n * p) : 0.f);
-    if (cost < least) {
-      least = cost;
-      best = p;
-    }
-  }
+  for (int32_t p = 2; p <= kPagedMaxParts; ++p)
+    if (paged_part_cost(n, p, chain, piece) < paged_part_cost(n, best, chain, piece)) best = p;
   return best;
 }
 

@@ -113,6 +113,23 @@ def test_against_oracle(gpu, case, hm):
     run_case(*case, hm=hm, seed=len(case[0]))
 
 
+# row blocks in many parts, of few and of many rows side by side
+PARTS = [
+    ([20000], [20], 16, 4, 1, 64, BF),
+    ([9000, 2], [16, 2], 64, 8, 1, 128, BF),
+    ([40, 3000, 6000, 1], [40, 1, 150, 1], 16, 8, 2, 128, BF),
+    ([3000, 2999], [1, 90], 16, 7, 7, 64, BF),
+    ([5000], [300], 32, 2, 1, 64, F32),
+    ([130, 1300], [130, 300], 16, 4, 4, 128, F32),
+]
+
+
+@pytest.mark.parametrize("case", PARTS, ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_parts(gpu, case, causal):
+    run_case(*case, causal=causal)
+
+
 @pytest.mark.parametrize("case", CASES, ids=str)
 def test_loose_bound(gpu, case):
     """A max_seqlen_k far above the lengths (a context's, say), which chooses another way to share the work."""
