@@ -215,7 +215,7 @@ def _qk(q, k, positions, params):
 def _out(t, like, name):
     """`t`, or a new contiguous tensor of the shape of `like`."""
     if t is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     B._need(t, name, like.dtype, 3)
     if t.shape != like.shape:
         raise ValueError(f"{name} must have the shape {tuple(like.shape)}")
@@ -249,13 +249,13 @@ def alloc_qk_workspace(q, k) -> torch.Tensor:
     return torch.empty(bs_qk_norm_rope_workspace_size(dims), dtype=torch.uint8, device=q.device)
 
 
-def _dweight(given, w, name, d, device):
+def _dweight(given, w, name, d):
     if w is None:
         if given is not None:
             raise ValueError(f"{name}: the gradient of a weight that the params do not have")
         return None
     if given is None:
-        return torch.empty(d, dtype=torch.float32, device=device)
+        return torch.empty_like(w, dtype=torch.float32)
     B._need(given, name, torch.float32, 1)
     if given.shape[0] != d:
         raise ValueError(f"{name} must have {d} elements")
@@ -272,16 +272,16 @@ def bs_qk_norm_rope_bwd(q, k, positions, params: QkParams, dq_out, dk_out, dq=No
     B._need(dq_out, "dq_out", dt, 3)
     B._need(dk_out, "dk_out", dt, 3)
     if dq is None:
-        dq = torch.empty((T, hq, d), dtype=dt, device=q.device)
+        dq = torch.empty_like(dq_out)
     if dk is None:
-        dk = torch.empty((T, hkv, d), dtype=dt, device=q.device)
+        dk = torch.empty_like(dk_out)
     dqs, q_shape = _heads(dq, "dq", dt)
     dks, k_shape = _heads(dk, "dk", dt)
     if q_shape != (T, hq, d) or k_shape != (T, hkv, d) or dq_out.shape != q_shape or dk_out.shape != k_shape:
         raise ValueError("dq_out, dk_out, dq and dk must have the shapes of q and k")
     _, wq, wk = params.tensors
-    dq_weight = _dweight(dq_weight, wq, "dq_weight", d, params.device)
-    dk_weight = _dweight(dk_weight, wk, "dk_weight", d, params.device)
+    dq_weight = _dweight(dq_weight, wq, "dq_weight", d)
+    dk_weight = _dweight(dk_weight, wk, "dk_weight", d)
     if workspace is None and (wq is not None or wk is not None):
         workspace = alloc_qk_workspace(q, k)
     _one_device(q.get_device(), k, positions, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace)

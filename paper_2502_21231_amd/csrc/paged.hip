@@ -21,10 +21,10 @@
 // shapes are known on the host, so a captured call can be replayed with other lengths.
 //
 // Measured: 32 single queries over up to 8K keys, 64/8 heads of 128, bf16: 80 us, 5.4 TB/s (the merge 4 of it); 256 over
-// up to 4K, 32/8: 307 us, 6.1 TB/s; one over 16K, 32/8: 14 us, two launches of which nothing fills the chip.  8 chunks
+// up to 4K, 32/8: 307 us, 6.1 TB/s; one over 3K, 32/8: 13 us, two launches that leave the chip empty.  8 chunks
 // of up to 1,024 queries over up to 16K keys, 64/8: 1.53 to 1.60 ms, 1,000 to 1,040 TFLOP/s of visible pairs, within
 // 4 % of the contiguous forward.  A chunk of 509 among 16 single queries over 8K, 48/8: 92 us, of which the keys' bytes
-// alone are 56.  float32, 3 x up to 200 queries over 700, 8/4 heads of 64: 19 us, a chain of key blocks and a merge.
+// alone are 56.  float32, 3 x up to 200 queries over 700, 8/4 heads of 64: 18 us, a chain of key blocks and a merge.
 //
 // Pages.  A wave copies 16 neighbouring keys at a time, which lie in one page (page_size is a multiple
 // of 16), so a page's place is scalar work, one number of the table per 16 keys, read a tile ahead.
@@ -940,18 +940,31 @@ void paged_kernel(const PagedParams p) {
   }
 }
 
-// Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, D/4 lanes per
-// row: by ranges of the line, or by row blocks.  Each lane weighs every D/4-th piece, so that no lane waits
-// for the pieces one after another.
+// Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, by ranges of the line, or by
+// row blocks.  D/4 lanes hold a row, as `per` groups that share its pieces where there are many pieces and few rows.
+// A launch is a chain of loads (share, maxima, sums): a lane weighs every D/4-th piece of its group, so that no lane
+// waits for the pieces one after another, and the first sums are requested before the maxima are known.
 template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
-  constexpr int LPR = D / 4;
-  if (kMode != kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;  // (0 items if lengths are refused)
+  constexpr int LPR = D / 4, G = 256 / LPR, AHEAD = 4;
+  __shared__ __attribute__((aligned(16))) f32x4 acc[256];
+  __shared__ float sums[G];
   const PagedShare s = p.share[blockIdx.x];
+  if (kMode != kLine && blockIdx.x >= p.hdr->n_items * (unsigned)p.hkv) return;  // (0 items if lengths are refused)
   if (s.pieces == 0) return;
   const int ch = threadIdx.x % LPR, lane0 = threadIdx.x & 63 & ~(LPR - 1);
-  for (int row = blockIdx.y * (256 / LPR) + threadIdx.x / LPR; row < s.rows; row += gridDim.y * (256 / LPR)) {
+  int rows = G;  // at a time
+  if (s.pieces > 2 * AHEAD)  // (one query over 30K, 16 heads of one group: 47 -> 33 us)
+    while (rows > 1 && (rows >> 1) * (int)gridDim.y >= s.rows) rows >>= 1;
+  const int per = G / rows, grp = threadIdx.x / LPR / rows, sub = threadIdx.x / LPR % rows;
+  for (int r0 = blockIdx.y * rows; r0 < s.rows; r0 += gridDim.y * rows) {
+    const int row = min(r0 + sub, s.rows - 1);
     auto at = [&](int i) { return (int64_t)(i == 0 ? s.first : s.next + i * s.step) * p.bm + row; };
+    auto part = [&](int j) { return *reinterpret_cast<const f32x4*>(p.part + at(grp + j * per) * D + ch * 4); };
+    const int mine = grp < s.pieces ? (s.pieces - grp + per - 1) / per : 0;  // pieces of this group
+    f32x4 ahead[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) ahead[j] = j < mine ? part(j) : f32x4{};
     float M = -INFINITY;
     for (int i = ch; i < s.pieces; i += LPR) M = fmaxf(M, p.stat[at(i)].x);
 #pragma unroll
@@ -959,20 +972,36 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
     const float base = M == -INFINITY ? 0.f : M;
     float l = 0.f;
     f32x4 o = f32x4{};
-    for (int i0 = 0; i0 < s.pieces; i0 += LPR) {
+    for (int j0 = 0; j0 < mine; j0 += LPR) {
       float wgt = 0.f;
-      if (i0 + ch < s.pieces) {
-        const float2 st = p.stat[at(i0 + ch)];
+      if (j0 + ch < mine) {
+        const float2 st = p.stat[at(grp + (j0 + ch) * per)];
         wgt = fast_exp2(st.x - base);
         l += wgt * st.y;
       }
-      const int n = min(LPR, s.pieces - i0);
+      const int n = min(LPR, mine - j0);
+      int j = 0;
+      if (j0 == 0) {
+#pragma unroll
+        for (; j < AHEAD; ++j) o += __shfl(wgt, lane0 + j) * ahead[j];
+      }
 #pragma unroll 8
-      for (int i = 0; i < n; ++i)
-        o += __shfl(wgt, lane0 + i) * *reinterpret_cast<const f32x4*>(p.part + at(i0 + i) * D + ch * 4);
+      for (; j < n; ++j) o += __shfl(wgt, lane0 + j) * part(j0 + j);
     }
 #pragma unroll
     for (int off = 1; off < LPR; off <<= 1) l += __shfl_xor(l, off);
+    if (per > 1) {  // the groups' sums, in order
+      __syncthreads();
+      acc[threadIdx.x] = o;
+      if (ch == 0) sums[threadIdx.x / LPR] = l;
+      __syncthreads();
+      if (grp == 0)
+        for (int g = 1; g < per; ++g) {
+          o += acc[threadIdx.x + g * rows * LPR];
+          l += sums[sub + g * rows];
+        }
+    }
+    if (grp > 0 || r0 + sub >= s.rows) continue;
     o *= l > 0.f ? 1.f / l : 0.f;
     const uint32_t r = (uint32_t)(s.row0 + row);
     const int qi = (int)(r / (uint32_t)p.group), head = s.hk * p.group + (int)r - qi * p.group;
