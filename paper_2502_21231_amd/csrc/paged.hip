@@ -716,7 +716,8 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
   Ops::load(qf, static_cast<const T*>(p.q) + row.at * D, hh);
   const int keys = e.lk;
   const int lim_lane = seen_by(p, e, row.qi) - hh * 4;
-  // keys some row sees, and this piece's end
+  // keys that all rows see; keys some row sees, and this piece's end
+  const int full = __builtin_amdgcn_readfirstlane(seen_by(p, e, (int)((uint32_t)(e.rb * BM) / (uint32_t)p.group)));
   int k_end = seen_by(p, e, (int)((uint32_t)(e.rb * BM + e.rows - 1) / (uint32_t)p.group));
   if (e.kb + e.n < e.v) k_end = min(k_end, (e.kb + e.n) * BLK);
 
@@ -775,7 +776,7 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
       ahead = pages_of(next + BLK);
       copy(Kw, p.kc, now, next);
     }
-    if (k0 + KT > keys || p.causal) {
+    if (k0 + KT > full) {
       const int lim = lim_lane - k0;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
