@@ -84,6 +84,13 @@ constexpr int kShortKeys = 1024, kFewWhole = 8;
 // merge: 16 queries of 4 heads over 8K keys, 8 KV heads: 42 us from one block on, 31 from four).
 constexpr int kTileRange = 4;
 
+// Time of a key with its row block, two workgroups on a CU, us (at head_dim 128 and 64: a tile of 64 keys 2.1 and 1.2;
+// 128 keys in float32 5.8 and 4.6), and of a part's sums, written and read at 4 TB/s.
+__host__ __device__ constexpr float key_us(bool bf, int d) {
+  return bf ? (d == 128 ? 0.033f : 0.018f) : (d == 128 ? 0.045f : 0.036f);
+}
+__host__ __device__ constexpr float piece_us(bool bf, int d) { return (bf ? kTileBM : kFewBM) * d * 2e-6f; }
+
 // How the work of a call is shared: a line, or items in the tile or in the few form.
 enum Mode { kLine = 0, kTileItems = 1, kFewItems = 2 };
 
@@ -893,12 +900,8 @@ void paged_kernel(const PagedParams p) {
     Piece e;
     int32_t parts = 1;
     if (p.parts > 1) {
-      // time of a key with its row block (a tile of 64 keys 2.1 us at head_dim 128; 128 keys in float32 4.5), and
-      // of a part's sums, written and read at 4 TB/s
-      constexpr float us = (sizeof(T) == 2 ? 0.033f : 0.035f) * (D == 128 ? 1.f : 0.55f);
-      constexpr float piece = (sizeof(T) == 2 ? kTileBM : kFewBM) * D * 2e-6f;
       const int32_t keys = p.num_seqs <= 256 ? L.lk[0] : p.max_len;  // (the longest comes first)
-      parts = __builtin_amdgcn_readfirstlane(best_parts(line * p.hkv, (float)keys * us, piece));
+      parts = __builtin_amdgcn_readfirstlane(best_parts(line * p.hkv, (float)keys * key_us(sizeof(T) == 2, D), piece_us(sizeof(T) == 2, D)));
     }
     if (!item_piece<T, D, kMode>(p, L, line, blockIdx.x, parts, e)) return;
     if (p.parts > 1 && e.kb == 0 && threadIdx.x == 0)
@@ -944,10 +947,10 @@ void paged_kernel(const PagedParams p) {
 // Row blocks of several pieces: O = sum 2^(M_i - M) O_i / L, L = sum 2^(M_i - M) L_i, by ranges of the line, or by
 // row blocks.  D/4 lanes hold a row, as `per` groups that share its pieces where there are many pieces and few rows.
 // A launch is a chain of loads (share, maxima, sums): a lane weighs every D/4-th piece of its group, so that no lane
-// waits for the pieces one after another, and the first sums are requested before the maxima are known.
+// waits for the pieces one after another, and sums are requested four at a time (eight: 1 us more where row blocks have two or three), the first before the maxima are known.
 template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
-  constexpr int LPR = D / 4, G = 256 / LPR, AHEAD = 4;
+  constexpr int LPR = D / 4, G = 256 / LPR, AT_ONCE = 4;
   __shared__ __attribute__((aligned(16))) f32x4 acc[256];
   __shared__ float sums[G];
   const PagedShare s = p.share[blockIdx.x];
@@ -955,39 +958,45 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedParams p) {
   if (s.pieces == 0) return;
   const int ch = threadIdx.x % LPR, lane0 = threadIdx.x & 63 & ~(LPR - 1);
   int rows = G;  // at a time
-  if (s.pieces > 2 * AHEAD)  // (one query over 30K, 16 heads of one group: 47 -> 33 us)
+  if (s.pieces > 2 * AT_ONCE)  // (one query over 30K, 16 heads of one group: 47 -> 33 us)
     while (rows > 1 && (rows >> 1) * (int)gridDim.y >= s.rows) rows >>= 1;
   const int per = G / rows, grp = threadIdx.x / LPR / rows, sub = threadIdx.x / LPR % rows;
   for (int r0 = blockIdx.y * rows; r0 < s.rows; r0 += gridDim.y * rows) {
     const int row = min(r0 + sub, s.rows - 1);
-    auto at = [&](int i) { return (int64_t)(i == 0 ? s.first : s.next + i * s.step) * p.bm + row; };
-    auto part = [&](int j) { return *reinterpret_cast<const f32x4*>(p.part + at(grp + j * per) * D + ch * 4); };
+    // (2 kPagedSlots pieces of 128 rows: byte offsets of 32 bits, which take half the registers of pointers)
+    auto at = [&](int i) { return (uint32_t)(i == 0 ? s.first : s.next + i * s.step) * (uint32_t)p.bm + (uint32_t)row; };
+    auto part = [&](int j) {
+      const uint32_t off = (at(grp + j * per) * D + ch * 4) * 4u;
+      return *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.part) + off);
+    };
+    auto stat = [&](int i) { return *reinterpret_cast<const float2*>(reinterpret_cast<const char*>(p.stat) + at(i) * 8u); };
     const int mine = grp < s.pieces ? (s.pieces - grp + per - 1) / per : 0;  // pieces of this group
-    f32x4 ahead[AHEAD];
+    f32x4 x[AT_ONCE];
+    auto request = [&](int j0) {
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) ahead[j] = j < mine ? part(j) : f32x4{};
+      for (int j = 0; j < AT_ONCE; ++j) x[j] = j0 + j < mine ? part(j0 + j) : f32x4{};
+    };
+    request(0);
     float M = -INFINITY;
-    for (int i = ch; i < s.pieces; i += LPR) M = fmaxf(M, p.stat[at(i)].x);
+    for (int i = ch; i < s.pieces; i += LPR) M = fmaxf(M, stat(i).x);
 #pragma unroll
     for (int off = 1; off < LPR; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
     const float base = M == -INFINITY ? 0.f : M;
     float l = 0.f;
     f32x4 o = f32x4{};
-    for (int j0 = 0; j0 < mine; j0 += LPR) {
-      float wgt = 0.f;
-      if (j0 + ch < mine) {
-        const float2 st = p.stat[at(grp + (j0 + ch) * per)];
-        wgt = fast_exp2(st.x - base);
-        l += wgt * st.y;
+    float wgt = 0.f;  // of piece ch of LPR
+    for (int j0 = 0; j0 < mine; j0 += AT_ONCE) {
+      if (j0 % LPR == 0) {
+        wgt = 0.f;
+        if (j0 + ch < mine) {
+          const float2 st = stat(grp + (j0 + ch) * per);
+          wgt = fast_exp2(st.x - base);
+          l += wgt * st.y;
+        }
       }
-      const int n = min(LPR, mine - j0);
-      int j = 0;
-      if (j0 == 0) {
+      if (j0 > 0) request(j0);
 #pragma unroll
-        for (; j < AHEAD; ++j) o += __shfl(wgt, lane0 + j) * ahead[j];
-      }
-#pragma unroll 8
-      for (; j < n; ++j) o += __shfl(wgt, lane0 + j) * part(j0 + j);
+      for (int j = 0; j < AT_ONCE; ++j) o += __shfl(wgt, lane0 + j0 % LPR + j) * x[j];
     }
 #pragma unroll
     for (int off = 1; off < LPR; off <<= 1) l += __shfl_xor(l, off);
@@ -1046,7 +1055,11 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
     pieces = 2 * kPagedSlots;
   } else {
     const int64_t n = blocks(L.bm);
-    L.parts = n >= kPagedSlots || rows <= kFewBM * seqs ? 1 : kPagedMaxParts;
+    // (where about so many row blocks of the longest chains would not be cut, the merge need not be launched)
+    const int64_t about = (rows / L.bm > seqs ? rows / L.bm : rows < seqs ? rows : seqs) * d.hkv;
+    const bool whole = n >= kPagedSlots || rows <= kFewBM * seqs ||
+                       paged_parts((int32_t)about, max_seqlen_k * key_us(bf, d.head_dim), piece_us(bf, d.head_dim)) == 1;
+    L.parts = whole ? 1 : kPagedMaxParts;
     pieces = n * L.parts < 2 * kPagedSlots ? n * L.parts : 2 * kPagedSlots;  // (what paged_parts keeps to)
     L.grid = L.parts == 1 ? (int32_t)(n > 0 ? n : 1) : (int32_t)pieces;      // (one workgroup checks the lengths)
     L.shares = L.parts > 1 ? (int32_t)n : 0;

@@ -111,22 +111,30 @@ BS_HD int32_t paged_head(int64_t x, int32_t line) {
 }
 // Into how many parts the keys of n < kPagedSlots row blocks are cut, n times that at most 2 kPagedSlots: the
 // smallest estimate, in microseconds, of
-//   chain x rounds of workgroups / parts  +  5 for the merge's launch, 0.2 for each of a row block's parts, which it
+//   chain x rounds of workgroups / parts  +  3 for the merge's launch, 0.2 for each of a row block's parts, which it
 //   reads one after another, and `piece` for each part's sums,
 // the rounds between the whole number that equal chains take and what uneven ones, the longest first, take on
-// average.  chain: time of the longest.  Measured, us: one sequence of 512 new tokens over 14K, 64/8 heads (256 row
-// blocks): 2 parts 166, 4 parts 177; 700 over 9K, 48/8 (264): 1 part 160, 3 parts 134; 900 over 1K, 64/8 (450): 1
-// part 65, 2 parts 83; 128 over 16K, 64/8 (64): 4 parts 57, 8 parts 55; 300 over 60K, 8/2 (20): 8 parts 86, 45 63.
+// average; a workgroup that has its CU to itself takes two thirds of the time.  chain: time of the longest.  Measured,
+// us: one sequence of 512 new tokens over 14K, 64/8 heads (256 row blocks): 2 parts 166, 4 parts 177; 700 over 9K,
+// 48/8 (264): 1 part 160, 3 parts 134; 900 over 1K, 64/8 (450): 1 part 65, 2 parts 83; 128 over 16K, 64/8 (64): 4
+// parts 57, 8 parts 55; 300 over 60K, 8/2 (20): 8 parts 86, 45 63; a prompt of 700, 16/4 (88): 1 part 22, 2 parts 25.
 BS_HD float paged_part_cost(int32_t n, int32_t p, float chain, float piece) {
   if (p > 1 && n * p > 2 * kPagedSlots) return 1e30f;
   const float x = (float)(n * p) / kPagedSlots + 0.4f, even = x > 1.f ? x : 1.f;
   const float whole = (float)((n * p + kPagedSlots - 1) / kPagedSlots);
-  return chain * (0.7f * whole + 0.3f * even) / (float)p + (p > 1 ? 5.f + 0.2f * (float)p + piece * (float)(n * p) : 0.f);
+  const float rate = n * p <= kPagedSlots / 2 ? 0.66f : 1.f;
+  return chain * rate * (0.7f * whole + 0.3f * even) / (float)p + (p > 1 ? 3.f + 0.2f * (float)p + piece * (float)(n * p) : 0.f);
 }
 BS_HD int32_t paged_parts(int32_t n, float chain, float piece) {
   int32_t best = 1;
-  for (int32_t p = 2; p <= kPagedMaxParts; ++p)
-    if (paged_part_cost(n, p, chain, piece) < paged_part_cost(n, best, chain, piece)) best = p;
+  float least = paged_part_cost(n, 1, chain, piece);
+  for (int32_t p = 2; p <= kPagedMaxParts && n * p <= 2 * kPagedSlots; ++p) {
+    const float cost = paged_part_cost(n, p, chain, piece);
+    if (cost < least) {
+      least = cost;
+      best = p;
+    }
+  }
   return best;
 }
 
