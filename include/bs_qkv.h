@@ -97,7 +97,8 @@ int bs_kv_append(const bs_dims* dims, const bs_qk_params* params, const bs_paged
 
 /* Bytes of workspace of bs_attn_paged_fwd (0: invalid arguments).  It depends on dims, num_seqs and
  * max_seqlen_k only, needs no initialisation, and holds nothing across calls except what
- * bs_read_device_status() reads. */
+ * bs_read_device_status() reads.  A smaller call may need more than a larger one (its row blocks come in
+ * parts); 66 MiB are enough for every call. */
 size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32_t max_seqlen_k);
 
 /* Attention of the new tokens of each sequence (rows of q as in bs_kv_append; one, some or all of the

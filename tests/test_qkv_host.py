@@ -200,3 +200,18 @@ def test_binding_refuses_tensors_elsewhere():
     for index in (-1, 0):
         with pytest.raises(ValueError, match=On(index).device):
             Q._one_device(1, On(1), On(index))
+
+
+def test_one_workspace_can_serve_every_paged_call(lib):
+    most = 0
+    for dtype in (B.BS_BF16, B.BS_F32):
+        for d in (64, 128):
+            for hq, hkv in ((1, 1), (8, 1), (64, 8), (32, 32), (4096, 1), (4096, 4096)):
+                for T in (0, 1, 2, 7, 64, 300, 3000, 1 << 17):
+                    for n in (0, 1, 2, 9, 64, 16384):
+                        for keys in (0, 1, 200, 1025, 5000, 1 << 20, (1 << 30) - 1):
+                            size = lib.bs_attn_paged_workspace_size(
+                                ctypes.byref(dims(total_q=T, hq=hq, hkv=hkv, head_dim=d, dtype=dtype)), n, keys)
+                            assert size > 0
+                            most = max(most, size)
+    assert 64 << 20 < most <= 66 << 20
