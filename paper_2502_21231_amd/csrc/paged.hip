@@ -5,10 +5,10 @@
 // one.  A workgroup of four waves takes one of two forms for a block of rows:
 //   few   32 rows; the waves take 32 (bf16, head_dim 64: 64) keys in turn, each with LDS buffers, page
 //         numbers and a softmax of its own, joined at the end: bound by reading the keys, no barrier
-//         between copies (the layout of few_bf16.hip).  Sequences of up to 32 rows, and all float32
-//         ones, on the float32 matrix instruction;
-//   tile  bf16, 128 rows over tiles of 64 keys that the waves share, 32 rows each: bound by the matrix
-//         core (the layout of fwd_bf16.hip).
+//         between copies (the layout of few_bf16.hip).  Sequences of up to 32 rows; in float32, on that
+//         type's matrix instruction, longer ones too where there are not enough for tiles;
+//   tile  128 rows over tiles of 64 keys (float32: 32) that the waves share, 32 rows each: bound by the
+//         matrix core (the layout of fwd_bf16.hip).
 // Both side by side in one launch, so that a step of decoding and prompt chunks uses memory and matrix
 // core at once.  How the work is shared:
 //   line  the blocks of all sequences form one line cut into equal ranges (paged_plan.hpp): decoding,
@@ -78,7 +78,7 @@ struct PagedParams {
   float scale_log2;
 };
 
-constexpr int kTileBM = 128, kTileBN = 64, kFewBM = 32;
+constexpr int kTileBM = 128, kTileBN = 64, kTileBN32 = 32, kFewBM = 32;
 constexpr int kShortKeys = 1024, kFewWhole = 8;
 // Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
 // merge: 16 queries of 4 heads over 8K keys, 8 KV heads: 42 us from one block on, 31 from four).
@@ -105,9 +105,9 @@ struct Shape {
 };
 template <typename T, int D, int kMode>
 __device__ __forceinline__ Shape shape_of(const PagedSeg& s) {
-  if (kMode == kFewItems || sizeof(T) == 4 || (int64_t)s.lq * s.group <= kFewBM)
+  if (kMode == kFewItems || (sizeof(T) == 4 ? kMode != kTileItems : (int64_t)s.lq * s.group <= kFewBM))
     return Shape{kFewBM, 4 * few_keys<T, D>()};
-  return Shape{kTileBM, kTileBN};
+  return Shape{kTileBM, sizeof(T) == 4 ? kTileBN32 : kTileBN};
 }
 
 // What a workgroup knows of the segments: thread t takes segments t * n .. of n = ceil(num_seqs / 256), or with n = 1
@@ -432,8 +432,8 @@ __device__ __forceinline__ int own_thread() {
 
 // LDS of a workgroup: two arrays X and Y, so that the compiler can tell copies into one from reads of the other.
 // Tile form: X and Y are the two buffers, K then V in each; few form: X holds the waves' K, Y their V.
-template <typename T, int D>
-constexpr int buf_elems() { return sizeof(T) == 4 ? 128 * D : 128 * 128; }
+template <typename T, int D, int kMode>
+constexpr int buf_elems() { return sizeof(T) == 2 ? 128 * 128 : kMode == kTileItems ? 2 * kTileBN32 * D : 128 * D; }
 struct FewLds {
   float m[4][32], l[4][32];
 };
@@ -441,7 +441,7 @@ struct TileLds {
   __attribute__((aligned(16))) int32_t miss[2][4];  // per buffer and 16 keys: the page is not there
 };
 
-// Tile form (bf16).
+// Tile form of bf16.
 template <int D>
 __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e, bf16 (&X)[128 * 128],
                                            bf16 (&Y)[128 * 128], TileLds& S) {
@@ -705,6 +705,121 @@ struct FewOps<float, D> {
   }
 };
 
+// Tile form of float32: tiles of 32 keys, of which two waves copy K and two V, 16 keys each.  Half the LDS of the few
+// form, so that two workgroups share a CU at head_dim 128 too, and no sum over waves at the end.
+template <int D>
+__device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e, float (&X)[2 * kTileBN32 * D],
+                                           float (&Y)[2 * kTileBN32 * D], TileLds& S) {
+  typedef FewOps<float, D> Ops;
+  constexpr int BM = kTileBM, BN = kTileBN32, TILE = BN * D, DB = D / 32;
+  const int tid = own_thread();
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hh = lane >> 5;
+  const float c2 = p.scale_log2;
+  const int tstride = (int)p.token_stride;
+  const Ops ops(lane);
+  const int qrow = w * 32 + c;
+  const bool qvalid = qrow < e.rows;
+  const Row row = row_of(p, e, (uint32_t)(e.rb * BM + (qvalid ? qrow : 0)));
+  typename Ops::Q qf[Ops::NQ];
+  Ops::load(qf, static_cast<const float*>(p.q) + row.at * D, hh);
+  const int lim_base = seen_by(p, e, row.qi) - hh * 4;
+  const int full = seen_by(p, e, (int)((uint32_t)(e.rb * BM) / (uint32_t)p.group));
+  const int n_full = __builtin_amdgcn_readfirstlane(full > 0 ? full / BN : 0);  // tiles that all rows see whole
+  const int t0 = e.kb, n_tiles = e.kb + e.n, keys = e.lk;
+
+  const int32_t* table = p.table + e.seg * p.table_stride;
+  const int64_t hoff = e.hk * p.head_stride;
+  const int half = w & 1;
+  const char* cache = w < 2 ? p.kc : p.vc;
+  auto page_of = [&](int t) {
+    const int key = t * BN + half * 16, page = table[min(key, keys - 1) >> p.page_shift];
+    return key < keys ? page : -1;
+  };
+  auto copy = [&](int t, int page, float* buf, int32_t* miss) {
+    const int key = t * BN + half * 16;
+    page = __builtin_amdgcn_readfirstlane(page);
+    const bool there = page >= 0 && page < p.num_pages;
+    const int64_t off = page * p.page_stride + (int64_t)(key & ((1 << p.page_shift) - 1)) * tstride + hoff;
+    const char* src = there ? cache + off : reinterpret_cast<const char*>(g_zero_row);
+    const int last = min(15, keys - 1 - key);
+    copy16<D, 0>(buf + (w >> 1) * TILE + half * 16 * D, src, there ? tstride : 0, last < 0 ? 0 : last, lane);
+    if (w < 2 && lane == 0) miss[half] = !there && key < keys;
+  };
+
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+  float m2 = -INFINITY, l_run = 0.f;
+  copy(t0, keys > 0 ? page_of(t0) : -1, X, S.miss[0]);
+  int page = e.n > 1 ? page_of(t0 + 1) : -1;
+  wait_vmem_all();
+  __syncthreads();
+
+  const bool idle = w * 32 >= e.rows;  // a wave without rows copies only
+  auto step = [&](int t, const float* B, const int32_t* miss, float* Bn, int32_t* miss_n) {
+    if (t + 1 < n_tiles) {
+      copy(t + 1, page, Bn, miss_n);
+      page = page_of(t + 2);
+    }
+    if (!idle) {
+      f32x16 s[1];
+      ops.scores(B, qf, s);
+      if (t >= n_full) {
+        const int lim = lim_base - t * BN;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[0][r] = ((r >> 2) * 8 + (r & 3)) < lim ? s[0][r] : -INFINITY;
+      }
+      if (__builtin_amdgcn_readfirstlane(miss[0] | miss[1])) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[0][r] = miss[r >> 3] ? -INFINITY : s[0][r];
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[0][r]);
+      mx = half_max(mx) * c2;
+      if (__any(mx > m2)) {
+        const float m_new = fmaxf(m2, mx);
+        const float alpha = fast_exp2(m2 - (m_new == -INFINITY ? 0.f : m_new));
+        m2 = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      }
+      const float base = m2 == -INFINITY ? 0.f : m2;
+      typename Ops::P pr;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float ex = fast_exp2(fmaf(s[0][r], c2, -base));
+        l_run += ex;
+        Ops::put(pr, 0, r, ex);
+      }
+      ops.values(B + TILE, pr, oacc);
+    }
+    wait_vmem_all();
+    __syncthreads();
+  };
+  for (int t = t0; t < n_tiles; t += 2) {
+    step(t, X, S.miss[0], Y, S.miss[1]);
+    if (t + 1 < n_tiles) step(t + 1, Y, S.miss[1], X, S.miss[0]);
+  }
+
+  // (whole row blocks only: a call of this form has enough of them)
+  const float l_tot = half_sum(l_run);
+  if (!qvalid) return;
+  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float* op = static_cast<float*>(p.o) + row.at * D;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int i = (r >> 2) * 8 + hh * 4 + (r & 3);  // acc[.][r]: elements DB i ..
+    if constexpr (D == 128) {
+      *reinterpret_cast<f32x4*>(op + i * 4) = f32x4{oacc[0][r], oacc[1][r], oacc[2][r], oacc[3][r]} * inv;
+    } else if (r % 2 == 0) {
+      *reinterpret_cast<f32x4*>(op + i * 2) = f32x4{oacc[0][r], oacc[1][r], oacc[0][r + 1], oacc[1][r + 1]} * inv;
+    }
+  }
+  if (hh == 0) p.lse[row.head * p.total_q + e.q_start + row.qi] = lse_of(m2, l_tot);
+}
+
 // Few form.  kAux: cache policy of the copies (2: non-temporal).
 template <typename T, int D, int kAux, int N>
 __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, T (&X)[N], T (&Y)[N], FewLds& S) {
@@ -882,7 +997,7 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
 template <typename T, int D, int kMode>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_kernel(const PagedParams p) {
-  constexpr int N = buf_elems<T, D>();
+  constexpr int N = buf_elems<T, D, kMode>();
   __shared__ __attribute__((aligned(16))) T X[N];
   __shared__ __attribute__((aligned(16))) T Y[N];
   __shared__ PagedLds L;
@@ -895,7 +1010,9 @@ void paged_kernel(const PagedParams p) {
     return;
   }
   // non-temporal copies where a sequence's keys are read once
-  auto few = [&](const Piece& e) { few_piece<T, D, sizeof(T) == 2 ? 2 : 0>(p, e, X, Y, F); };
+  auto few = [&](const Piece& e) {
+    if constexpr (sizeof(T) == 2 || kMode != kTileItems) few_piece<T, D, sizeof(T) == 2 ? 2 : 0>(p, e, X, Y, F);
+  };
   if constexpr (kMode != kLine) {
     Piece e;
     int32_t parts = 1;
@@ -907,7 +1024,7 @@ void paged_kernel(const PagedParams p) {
     if (p.parts > 1 && e.kb == 0 && threadIdx.x == 0)
       p.share[e.at / parts] = PagedShare{e.pieces > 1 ? e.pieces : 0, e.at, e.at, 1, e.hk, e.rows,
                                            e.rb * (kMode == kFewItems ? kFewBM : kTileBM), e.q_start};
-    if (kMode == kFewItems || e.lq * p.group <= kFewBM) {
+    if (kMode == kFewItems || (sizeof(T) == 2 && e.lq * p.group <= kFewBM)) {
       few(e);
     } else {
       if constexpr (kMode != kFewItems) tile_piece<D>(p, e, X, Y, S);
@@ -1048,6 +1165,14 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   if (seqs == 0) L.mode = kLine;
   else if (rows <= kFewBM * seqs) L.mode = max_seqlen_k <= kFewWhole * few_block ? kFewItems : kLine;
   else if (!bf && rows <= 2 * kTileBM * seqs && (blocks(kFewBM) < kPagedSlots || max_seqlen_k > kShortKeys)) L.mode = kLine;
+  // Float32 tiles, where those fill the chip.  At head_dim 128 the few form has a CU's LDS to itself, and all it does
+  // before and after its products counts: 36 prompts of up to 154 tokens, 32/4 heads 180 -> 97 us, one of 4,096, 32/8
+  // 1.25 -> 1.13 ms.  A single query's chain of many keys is four times as long, though (a chunk of 2,000 among 32
+  // single queries over 4K, 32/8: 818 us without tiles, 1,015 with).  At head_dim 64 two workgroups of the few form
+  // share a CU, and tiles are ahead over few keys only: 36 x 154 80 -> 54 us, but 64 x 60 over 500 49 -> 63.
+  const bool short_chains = d.head_dim == 64 ? max_seqlen_k <= 256
+                                             : max_seqlen_k <= 2048 || rows >= 8 * kTileBM * seqs;
+  if (!bf && seqs > 0 && rows > kFewBM * seqs && blocks(kTileBM) >= kPagedSlots && short_chains) L.mode = kTileItems;
   L.bm = L.mode == kTileItems || (L.mode == kLine && bf && rows > kFewBM) ? kTileBM : kFewBM;
   int64_t pieces;
   if (L.mode == kLine) {
@@ -1136,7 +1261,7 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   do {                                                                                                  \
     if (W.mode == kLine) BS_LAUNCH(T, D, kLine);                                                        \
     else if (W.mode == kFewItems) BS_LAUNCH(T, D, kFewItems);                                           \
-    else if constexpr (sizeof(T) == 2) BS_LAUNCH(T, D, kTileItems);                                     \
+    else BS_LAUNCH(T, D, kTileItems);                                                                   \
   } while (0)
   if (d.dtype == BS_BF16) {
     if (d.head_dim == 128) BS_CALL(bf16, 128); else BS_CALL(bf16, 64);

@@ -124,6 +124,31 @@ PARTS = [
 ]
 
 
+# float32 with enough row blocks for the tile form: 512 of 128 rows over all KV heads
+TILES32 = [
+    ([130] * 20 + [1, 40], [130] * 20 + [1, 0], 16, 64, 16, 64, F32),
+    ([70, 33, 500, 5], [70, 33, 100, 9], 32, 256, 64, 128, F32),
+    ([250, 17], [250, 12], 16, 512, 128, 64, F32),
+    ([40, 97, 31], [40, 97, 31], 64, 192, 192, 128, F32),
+]
+
+
+@pytest.mark.parametrize("case", TILES32, ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+def test_float32_tiles(gpu, case, causal):
+    run_case(*case, causal=causal, pad=3)
+
+
+def test_float32_tiles_with_missing_pages(gpu):
+    def edit(kc, vc, table):
+        table[0, 2] = -1
+        table[1, 0] = 1 << 20
+        table[2, :] = -1
+
+    for d in (64, 128):
+        run_case([100, 40, 20], [100, 40, 20], 16, 512, 256, d, F32, edit=edit)
+
+
 @pytest.mark.parametrize("case", PARTS, ids=str)
 @pytest.mark.parametrize("causal", [True, False])
 def test_many_parts(gpu, case, causal):
