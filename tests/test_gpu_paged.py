@@ -239,6 +239,19 @@ def test_many_sequences(gpu):
     run_case(lens[:260], new[:260], 16, 8, 1, 64, BF, most=3000)
 
 
+def test_many_sequences_in_parts_and_float32_tiles(gpu):
+    """The same with row blocks in parts, with both forms among them, and as float32 tiles."""
+    rng = np.random.default_rng(1)
+    lens = [int(x) for x in rng.integers(0, 900, 300)]
+    new = [int(min(n, x)) for n, x in zip(lens, rng.integers(1, 5, 300))]
+    run_case(lens, new, 16, 16, 1, 64, BF, most=900)  # some 40 rows on average
+    run_case(lens, new, 16, 16, 1, 128, BF, most=100000, pad=5)
+    lens = [int(x) for x in rng.integers(0, 200, 290)]
+    new = [int(min(n, x)) for n, x in zip(lens, rng.integers(2, 9, 290))]
+    run_case(lens, new, 16, 16, 2, 64, F32)
+    run_case(lens, new, 32, 16, 2, 128, F32, causal=False)
+
+
 def test_refused_lengths_write_nothing(gpu):
     kc, vc, table = make_cache(0, [40, 40], 16, 2, 64, BF)
     q = rand(0, 1, (4, 4, 64), BF).cuda()
