@@ -21,7 +21,7 @@
 // shapes are known on the host, so a captured call can be replayed with other lengths.
 //
 // Measured: 32 single queries over up to 8K keys, 64/8 heads of 128, bf16: 80 us, 5.4 TB/s (the merge 4 of it); 256 over
-// up to 4K, 32/8: 307 us, 6.1 TB/s; one over 3K, 32/8: 13 us, two launches that leave the chip empty.  8 chunks
+// up to 4K, 32/8: 307 us, 6.1 TB/s; one over 3K, 32/8: 12 us, two launches that leave the chip empty.  8 chunks
 // of up to 1,024 queries over up to 16K keys, 64/8: 1.53 to 1.60 ms, 1,000 to 1,040 TFLOP/s of visible pairs, within
 // 4 % of the contiguous forward.  A chunk of 509 among 16 single queries over 8K, 48/8: 92 us, of which the keys' bytes
 // alone are 56.  float32, 3 x up to 200 queries over 700, 8/4 heads of 64: 18 us, a chain of key blocks and a merge.
@@ -80,9 +80,6 @@ struct PagedParams {
 
 constexpr int kTileBM = 128, kTileBN = 64, kTileBN32 = 32, kFewBM = 32;
 constexpr int kShortKeys = 1024, kFewWhole = 8;
-// Key blocks of a range at least, where some are tiles (the sums that a shared tile leaves are as long to write and
-// merge: 16 queries of 4 heads over 8K keys, 8 KV heads: 42 us from one block on, 31 from four).
-constexpr int kTileRange = 4;
 
 // Time of a key with its row block, two workgroups on a CU, us (at head_dim 128 and 64: a tile of 64 keys 2.1 and 1.2;
 // 128 keys in float32 5.8 and 4.6), and of a part's sums, written and read at 4 TB/s.
@@ -115,7 +112,7 @@ __device__ __forceinline__ Shape shape_of(const PagedSeg& s) {
 struct PagedLds {
   int32_t pre[257];  // places on the line before each thread's segments, per KV head
   int32_t sum[4];
-  int32_t bad, tiles;
+  int32_t bad;
   __attribute__((aligned(16))) int32_t seg[256], q0[256], lq[256], lk[256];  // n = 1: the segment, its first query and lengths
 };
 
@@ -156,10 +153,7 @@ template <typename T, int D, int kMode>
 __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int32_t pt = seqs_per_thread(p.num_seqs);
-  if (tid == 0) {
-    L.bad = BS_DEV_OK;
-    L.tiles = 0;
-  }
+  if (tid == 0) L.bad = BS_DEV_OK;
   int32_t code = BS_DEV_OK;
   if (tid == 0) {
     const int32_t first = p.cu_q[0], end = p.cu_q[p.num_seqs];
@@ -178,10 +172,8 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
     return c == BS_DEV_OK ? PagedSeg{(int32_t)n, len, p.group, p.causal} : PagedSeg{0, 0, p.group, p.causal};
   };
   int32_t sum = 0;
-  bool tiles = false;
   auto count = [&](const PagedSeg& s) {
     if (s.lq > 0) sum += segment_cost<T, D, kMode>(s);
-    tiles |= s.lq > 0 && shape_of<T, D, kMode>(s).bm == kTileBM;
   };
   if (pt > 1) {
     for (int32_t b = tid * pt; b < min(tid * pt + pt, p.num_seqs); ++b) {
@@ -224,7 +216,6 @@ __device__ __forceinline__ int32_t paged_line(const PagedParams& p, PagedLds& L)
     if (tid == 0) L.bad = code;
     else atomicCAS(&L.bad, BS_DEV_OK, code);
   }
-  if (tiles) L.tiles = 1;
   int32_t at = run - sum;
   for (int i = 0; i < w; ++i) at += L.sum[i];
   L.pre[tid] = at;
@@ -1031,7 +1022,7 @@ void paged_kernel(const PagedParams p) {
     }
   } else {
     PagedShare* share = p.share + blockIdx.x;
-    const PagedRanges R((int64_t)line * p.hkv, __builtin_amdgcn_readfirstlane(L.tiles) ? kTileRange : 1);
+    const PagedRanges R((int64_t)line * p.hkv);
     const int32_t range = paged_range_of(blockIdx.x, R.n);
     bool left_share = false;
     if (range >= 0) {
@@ -1155,16 +1146,21 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   const bool bf = d.dtype == BS_BF16;
   auto blocks = [&](int bm) { return (rows / bm + (rows < seqs ? rows : seqs)) * d.hkv; };  // at most
   const int few_block = 4 * (bf && d.head_dim == 64 ? 64 : 32);
-  // Up to 32 rows per sequence on average: the line, unless all sequences are so short (kFewWhole key blocks) that
-  // what a workgroup saves by an equal share is less than the merge's launch.  More rows: items (measured, us, line /
-  // items: a chunk of 500 and 32 single queries over 8K, 64/8 heads 167 / 151; of 900 and 64 over 4K, 32/8 148 / 113;
-  // 8 x 30 over 4K, 64/8 44 / 38; but 32 x 30 over 8K 164 / 207, where chains are uneven).  In float32 up to 256 rows
-  // per sequence take the line where there are fewer row blocks than workgroups (a chunk of 300 and 32 single queries
-  // over 4K, 32/4, head_dim 64: 72 / 104) or keys are many.
-  L.mode = bf ? kTileItems : kFewItems;
+  // Up to 32 rows per sequence on average: where all sequences are short (kFewWhole key blocks), whole row blocks in
+  // the few form, since what a workgroup saves by an equal share is less than the merge's launch; the line for decoding
+  // (up to two new tokens per sequence on average; in bf16 more are ahead as items, measured in us, line / items: a
+  // chunk of 200 and 16 single queries over 3K, 32/32 heads 84 / 73; of 100 and 16 over 2K, 8/2 26 / 16; 6 queries of
+  // one sequence over 16K, 32/8 22 / 17; but 16 x 8 over 8K 54 / 56).  More rows: items (a chunk of 500 and 32 single
+  // queries over 8K, 64/8 heads 167 / 151; of 900 and 64 over 4K, 32/8 148 / 113; 8 x 30 over 4K, 64/8 44 / 38; but
+  // 32 x 30 over 8K 164 / 207, where chains are uneven).  In float32 up to 256 rows per sequence take the line where
+  // there are fewer row blocks than workgroups (a chunk of 300 and 32 single queries over 4K, 32/4, head_dim 64: 72 /
+  // 104) or keys are many.
+  const bool few = rows <= kFewBM * seqs, short_keys = max_seqlen_k <= kFewWhole * few_block;
+  const bool line32 = few || (rows <= 2 * kTileBM * seqs && (blocks(kFewBM) < kPagedSlots || max_seqlen_k > kShortKeys));
   if (seqs == 0) L.mode = kLine;
-  else if (rows <= kFewBM * seqs) L.mode = max_seqlen_k <= kFewWhole * few_block ? kFewItems : kLine;
-  else if (!bf && rows <= 2 * kTileBM * seqs && (blocks(kFewBM) < kPagedSlots || max_seqlen_k > kShortKeys)) L.mode = kLine;
+  else if (few && short_keys) L.mode = kFewItems;
+  else if (bf) L.mode = few && d.total_q <= 2 * seqs ? kLine : kTileItems;
+  else L.mode = line32 ? kLine : kFewItems;
   // Float32 tiles, where those fill the chip.  At head_dim 128 the few form has a CU's LDS to itself, and all it does
   // before and after its products counts: 36 prompts of up to 154 tokens, 32/4 heads 180 -> 97 us, one of 4,096, 32/8
   // 1.25 -> 1.13 ms.  A single query's chain of many keys is four times as long, though (a chunk of 2,000 among 32
@@ -1172,7 +1168,7 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   // share a CU, and tiles are ahead over few keys only: 36 x 154 80 -> 54 us, but 64 x 60 over 500 49 -> 63.
   const bool short_chains = d.head_dim == 64 ? max_seqlen_k <= 256
                                              : max_seqlen_k <= 2048 || rows >= 8 * kTileBM * seqs;
-  if (!bf && seqs > 0 && rows > kFewBM * seqs && blocks(kTileBM) >= kPagedSlots && short_chains) L.mode = kTileItems;
+  if (!bf && seqs > 0 && !few && blocks(kTileBM) >= kPagedSlots && short_chains) L.mode = kTileItems;
   L.bm = L.mode == kTileItems || (L.mode == kLine && bf && rows > kFewBM) ? kTileBM : kFewBM;
   int64_t pieces;
   if (L.mode == kLine) {
@@ -1182,7 +1178,7 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
     const int64_t n = blocks(L.bm);
     // (where about so many row blocks of the longest chains would not be cut, the merge need not be launched)
     const int64_t about = (rows / L.bm > seqs ? rows / L.bm : rows < seqs ? rows : seqs) * d.hkv;
-    const bool whole = n >= kPagedSlots || rows <= kFewBM * seqs ||
+    const bool whole = n >= kPagedSlots || (few && short_keys) ||
                        paged_parts((int32_t)about, max_seqlen_k * key_us(bf, d.head_dim), piece_us(bf, d.head_dim)) == 1;
     L.parts = whole ? 1 : kPagedMaxParts;
     pieces = n * L.parts < 2 * kPagedSlots ? n * L.parts : 2 * kPagedSlots;  // (what paged_parts keeps to)

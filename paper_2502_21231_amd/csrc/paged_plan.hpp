@@ -77,22 +77,13 @@ BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
 // Workgroups that run at a time (two per CU), the ranges of a line at most, and parts of a row block's keys at most.
 constexpr int32_t kPagedSlots = 512, kPagedMaxParts = 64;
 
-// The n <= kPagedSlots ranges of a line of `all` places, of `least` or more places each (one range: all), as equal as
-// can be.  A line has less than 2^31 places per KV head and less than 2^39 in all: the entry point refuses more.
+// The n <= kPagedSlots ranges of a line of `all` places, as equal as can be.  A line has less than 2^31 places per KV
+// head and less than 2^39 in all: the entry point refuses more.
 struct PagedRanges {
   int64_t all;
   int32_t n;
-  BS_HD PagedRanges(int64_t places, int32_t least) : all(places) {
-    n = kPagedSlots;
-    if (all < (int64_t)kPagedSlots * least) {
-      n = (int32_t)all / least;
-      if (n < 1) n = all > 0 ? 1 : 0;
-    }
-  }
-  BS_HD int64_t start(int32_t w) const {
-    if (n == kPagedSlots) return w * all / kPagedSlots;  // (a shift)
-    return n > 0 ? (uint32_t)w * (uint32_t)all / (uint32_t)n : 0;
-  }
+  BS_HD explicit PagedRanges(int64_t places) : all(places), n(places < kPagedSlots ? (int32_t)places : kPagedSlots) {}
+  BS_HD int64_t start(int32_t w) const { return n == kPagedSlots ? w * all / kPagedSlots : w; }  // (a shift)
   // The range that place x lies in (a float quotient is off by one at most).
   BS_HD int32_t of(int64_t x) const {
     int32_t w = (int32_t)((float)(x + 1) * (float)n / (float)all);

@@ -42,17 +42,17 @@ static void segment(const PagedSeg& s, int BM, int BLK) {
   if (c.n == 1) CHECK(c.start(1) == need);
 }
 
-static void ranges(const PagedRanges& R, int least) {
+static void ranges(const PagedRanges& R) {
   CHECK(R.n <= kPagedSlots && (R.n > 0) == (R.all > 0) && R.start(0) == 0 && (R.n == 0 || R.start(R.n) == R.all));
   for (int32_t w = 0; w < R.n; ++w) {
     const int64_t a = R.start(w), b = R.start(w + 1);
-    CHECK(b > a && (b - a >= least || R.n == 1) && b - a <= R.all / R.n + 1);
+    CHECK(b > a && b - a <= R.all / R.n + 1);
     CHECK(R.of(a) == w && R.of(b - 1) == w);
   }
 }
 
 // Segments of up to 32 rows take the first shape, others the second.
-static void line(const std::vector<PagedSeg>& segs, int hkv, int least) {
+static void line(const std::vector<PagedSeg>& segs, int hkv) {
   const int bm[2] = {32, 128}, blk[2] = {128, 64};
   auto kind = [&](const PagedSeg& s) { return (int64_t)s.lq * s.group <= 32 ? 0 : 1; };
   int64_t per_head = 0;
@@ -62,8 +62,8 @@ static void line(const std::vector<PagedSeg>& segs, int hkv, int least) {
     const int t = kind(s);
     if (s.lq > 0) per_head += paged_cost(s, bm[t], blk[t]).start(paged_row_blocks(s, bm[t]));
   }
-  const PagedRanges R(per_head * hkv, least);
-  ranges(R, least);
+  const PagedRanges R(per_head * hkv);
+  ranges(R);
   std::vector<int> taken(kPagedSlots, 0);
   for (int32_t b = 0; b < kPagedSlots; ++b) {
     const int32_t w = paged_range_of(b, R.n);
@@ -118,12 +118,12 @@ int main() {
     std::vector<PagedSeg> segs(rng() % 20);
     const int32_t group = pick(1, 16), causal = rng() % 4 != 0;
     for (PagedSeg& s : segs) s = PagedSeg{(int32_t)(rng() % 5 ? pick(1, 300) : 0), pick(1, 3000) - 1, group, causal};
-    line(segs, 1 + rng() % 9, 1 + n % 5);
+    line(segs, 1 + rng() % 9);
   }
   for (int64_t all : {(int64_t)0, (int64_t)1, (int64_t)511, (int64_t)512, (int64_t)513, ((int64_t)1 << 39) - 1})
     for (int n = 0; n < 2000; ++n) {
-      const PagedRanges R(all - n * (all >> 12), 1 + n % 5);
-      ranges(R, 1 + n % 5);
+      const PagedRanges R(all - n * (all >> 12));
+      ranges(R);
     }
   for (int n = 0; n < 300000; ++n) {
     const int32_t len = pick(1, (1 << 30)), h = rng() % 4096;

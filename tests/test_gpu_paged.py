@@ -133,6 +133,20 @@ TILES32 = [
 ]
 
 
+# decoding with a chunk among many single queries, whose work lies on one line
+LINES = [
+    ([2500] + [1300] * 39, [40] + [1] * 39, 16, 4, 2, 128, BF),
+    ([90 * i for i in range(60)], [0] + [1] * 58 + [60], 32, 3, 3, 64, BF),
+    ([1100, 3000, 2, 0], [1, 2, 2, 0], 16, 64, 1, 64, BF),
+]
+
+
+@pytest.mark.parametrize("case", LINES, ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+def test_decoding_with_a_chunk(gpu, case, causal):
+    run_case(*case, causal=causal, pad=1)
+
+
 @pytest.mark.parametrize("case", TILES32, ids=str)
 @pytest.mark.parametrize("causal", [True, False])
 def test_float32_tiles(gpu, case, causal):
