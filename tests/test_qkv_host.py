@@ -158,7 +158,7 @@ def test_paged_attention_refusals(lib):
     said(BAD, paged(lib, scale=0.0), "scale")
     said(UNS, paged(lib, dims(total_q=1 << 20, hq=4096, hkv=4096)), "total_q * hq")
     big = cache(max_pages=1 << 20, table_stride=1 << 20, page_size=1024, head_stride=64, token_stride=64)
-    said(UNS, paged(lib, dims(total_q=1 << 19, hq=2, hkv=2), c=big, n=16384, most=(1 << 30) - 1, q=1 << 45, out=1 << 46),
+    said(UNS, paged(lib, dims(total_q=1 << 15, hq=2, hkv=2), c=big, n=16384, most=(1 << 30) - 1, q=1 << 45, out=1 << 46),
          "too many for one call")
     said(BAD, paged(lib, out=None), "out is NULL")
     said(BAD, paged(lib, out=Q_AT), "out overlaps q")
