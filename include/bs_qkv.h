@@ -6,7 +6,7 @@
  *
  * Conventions are those of bs_attn.h (device pointers owned by the caller, no allocation, asynchronous
  * on `stream`, a status and bs_last_error() for what the host can check, BS_BF16 or BS_F32 data with
- * float32 arithmetic rounded once on the store, head_dim 64 or 128), and:
+ * float32 arithmetic rounded once on the store, but where a call says otherwise, head_dim 64 or 128), and:
  *   - dims->total_q is the number of tokens T; dims->total_k is not used.
  *   - "strided" operands [T, heads, head_dim] have contiguous heads (heads x head_dim elements) and
  *     `stride` elements from one token to the next: at least heads x head_dim, a multiple of 16 bytes.
@@ -107,6 +107,9 @@ size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32
  * contiguous; writes out [T, hq, head_dim] and lse [hq, T]; a row that sees no key gets out = 0,
  * lse = -inf.  Rows from cu_seqlens_q[num_seqs] on are left as they were.  What the pages hold behind
  * a sequence's last token is not looked at (it may be NaN).
+ *   - bf16: a sequence of more than 32 rows (queries x heads of a KV group) has its probabilities rounded to
+ *     bf16 before their product with V, as in bs_attn_varlen_fwd; of up to 32 rows they are within 2^-17.  LSE
+ *     is that of the unrounded ones.
  *   - max_seqlen_k (below 2^30) bounds kv_lens.  num_seqs is at most 16,384, T hq below 2^31; sizes whose
  *     work cannot be numbered in 32 bits (some 2^31 blocks of 128 rows and 64 keys per KV head) are
  *     refused with BS_ERR_UNSUPPORTED.  lse overlaps no other operand either.

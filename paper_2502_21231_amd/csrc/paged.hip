@@ -540,7 +540,10 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
       for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     }
     const float base = m2 == -INFINITY ? 0.f : m2;
-    bf16x8 pb[4];  // P rounded to bf16 for the product; the sum takes it in float32
+    // P rounded to bf16 for the product, as in the contiguous forward (the sum takes it in float32): a second product for
+    // what the rounding loses, as the few form has it, takes 37 % more (8 chunks of up to 1,024 queries over up to 16K keys,
+    // 64/8 heads 1,547 -> 2,111 us) for a relative error of 2.3e-3 -> 1.66e-3, of which the result's own rounding is 1.65e-3
+    bf16x8 pb[4];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -640,11 +643,18 @@ struct FewOps<bf16, D> {
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[kk], s[kb], 0, 0, 0);
       }
   }
-  // P rounded to bf16 for the product (the sum takes it in float32)
+  // P as two bf16 numbers, what the first loses by its rounding being the second: within 2^-17 of float32.  The few form
+  // waits for keys, so the second product costs little (32 single queries over up to 8K keys, 64/8 heads 78.3 -> 79.1 us;
+  // 256 over up to 4K, 32/8 300 -> 304; head_dim 64, 32 over 8K 51.1 -> 52.3), and the result's own rounding is all that
+  // is left of bf16 (relative error of those 32 2.1e-3 -> 1.65e-3).
   struct P {
-    bf16x8 x[2 * KB];
+    bf16x8 x[2 * KB], y[2 * KB];
   };
-  static __device__ __forceinline__ void put(P& p, int kb, int r, float v) { p.x[kb * 2 + (r >> 3)][r & 7] = f2bf(v); }
+  static __device__ __forceinline__ void put(P& p, int kb, int r, float v) {
+    const bf16 x = f2bf(v);
+    p.x[kb * 2 + (r >> 3)][r & 7] = x;
+    p.y[kb * 2 + (r >> 3)][r & 7] = f2bf(v - bf2f(x));
+  }
   __device__ __forceinline__ void values(const bf16* V, const P& p, f32x16 (&o)[DB]) const {
 #pragma unroll
     for (int ks = 0; ks < 2 * KB; ++ks)
@@ -652,6 +662,7 @@ struct FewOps<bf16, D> {
       for (int db = 0; db < DB; ++db) {
         const bf16x8 a = lds_tr16(V, (tbase ^ (db << 6)) + ks * 32 * D, (tbase ^ ((db << 6) | 32)) + ks * 32 * D + 16 * D);
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p.x[ks], o[db], 0, 0, 0);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p.y[ks], o[db], 0, 0, 0);
       }
   }
   static __device__ __forceinline__ void put_rows(bf16* K, bf16* V, int lane, const f32x16 (&o)[DB]) {
