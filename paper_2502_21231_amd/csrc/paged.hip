@@ -413,6 +413,29 @@ __device__ __forceinline__ int seen_by(const PagedParams& p, const Piece& e, int
 
 constexpr float kRescaleBy = 8.0f;  // log2 units (fwd_bf16.hip)
 
+// A lane's sum of weights, of which there may be millions of nearly one size: added one after another to a sum far above
+// them, all would be rounded the same way (131,072 keys 3 to 7 below a first one, in one chain: LSE off by 8.5e-4; so by
+// 1.9e-6).  A tile's weights make four sums, which are one addition, whose rounding the next one takes back.
+struct WeightSum {
+  float sum = 0.f, over = 0.f;  // over: what the last addition was rounded up by
+  float tile[4];
+  // weight i of a tile, in order
+  __device__ __forceinline__ void take(int i, float w) {
+    if (i == 0) tile[0] = w - over;
+    else if (i < 4) tile[i] = w;
+    else tile[i & 3] += w;
+  }
+  __device__ __forceinline__ void finish() {
+    const float x = (tile[0] + tile[1]) + (tile[2] + tile[3]), s = sum + x;
+    over = (s - sum) - x;
+    sum = s;
+  }
+  __device__ __forceinline__ void scale(float by) {
+    sum *= by;
+    over *= by;
+  }
+};
+
 // The thread's number, which the compiler does not know to be the same for every piece: what depends on it is
 // worked out in each (held over the loop of pieces, 46 registers of the line kernel spill).
 __device__ __forceinline__ int own_thread() {
@@ -481,7 +504,8 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   f32x16 oacc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-  float m2 = -INFINITY, l_run = 0.f;
+  float m2 = -INFINITY;
+  WeightSum l_run;
 
   copy(t0, keys > 0 ? page_of(t0) : -1, X, X + TILE, S.miss[0]);
   int page = e.n > 1 ? page_of(t0 + 1) : -1;
@@ -535,7 +559,7 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
       const float m_new = fmaxf(m2, mx);
       const float alpha = fast_exp2(m2 - (m_new == -INFINITY ? 0.f : m_new));
       m2 = m_new;
-      l_run *= alpha;
+      l_run.scale(alpha);
 #pragma unroll
       for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     }
@@ -549,10 +573,11 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float ex = fast_exp2(fmaf(sacc[kb][r], c2, -base));
-        l_run += ex;
+        l_run.take(kb * 16 + r, ex);
         pb[kb * 2 + (r >> 3)][r & 7] = f2bf(ex);
       }
     }
+    l_run.finish();
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
@@ -588,7 +613,7 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   const bf16* Z = two ? Y : X;
   step(std::false_type{}, n_tiles - 1, Z, Z + TILE, S.miss[two], nullptr, nullptr, nullptr);
 
-  const float l_tot = half_sum(l_run);
+  const float l_tot = half_sum(l_run.sum);
   if (!qvalid) return;
   uint32_t r1 = r_lane;
   asm volatile("" : "+v"(r1));  // the row's place is worked out again: held over the loop, registers spill
@@ -751,7 +776,8 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   f32x16 oacc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-  float m2 = -INFINITY, l_run = 0.f;
+  float m2 = -INFINITY;
+  WeightSum l_run;
   copy(t0, keys > 0 ? page_of(t0) : -1, X, S.miss[0]);
   int page = e.n > 1 ? page_of(t0 + 1) : -1;
   wait_vmem_all();
@@ -783,7 +809,7 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
         const float m_new = fmaxf(m2, mx);
         const float alpha = fast_exp2(m2 - (m_new == -INFINITY ? 0.f : m_new));
         m2 = m_new;
-        l_run *= alpha;
+        l_run.scale(alpha);
 #pragma unroll
         for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
       }
@@ -792,9 +818,10 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float ex = fast_exp2(fmaf(s[0][r], c2, -base));
-        l_run += ex;
+        l_run.take(r, ex);
         Ops::put(pr, 0, r, ex);
       }
+      l_run.finish();
       ops.values(B + TILE, pr, oacc);
     }
     wait_vmem_all();
@@ -806,7 +833,7 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   }
 
   // (whole row blocks only: a call of this form has enough of them)
-  const float l_tot = half_sum(l_run);
+  const float l_tot = half_sum(l_run.sum);
   if (!qvalid) return;
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
   float* op = static_cast<float*>(p.o) + row.at * D;
@@ -883,7 +910,8 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
   f32x16 oacc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-  float m2 = -INFINITY, l_run = 0.f;
+  float m2 = -INFINITY;
+  WeightSum l_run;
 
   int k0 = (e.kb * 4 + w) * KT;
   Place now;
@@ -925,7 +953,7 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
       const float m_new = fmaxf(m2, mx);
       const float alpha = fast_exp2(m2 - (m_new == -INFINITY ? 0.f : m_new));
       m2 = m_new;
-      l_run *= alpha;
+      l_run.scale(alpha);
 #pragma unroll
       for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     }
@@ -936,9 +964,10 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float ex = fast_exp2(fmaf(s[kb][r], c2, -base));
-        l_run += ex;
+        l_run.take(kb * 16 + r, ex);
         Ops::put(pr, kb, r, ex);
       }
+    l_run.finish();
     // V has landed.  (K's copies and the pages' load come after it; where the load is moved, waiting for
     // one operation more than needed is all that happens.)
     wait_copies<more() ? Ops::COPIES : 0>();
@@ -960,7 +989,7 @@ __device__ __forceinline__ void few_piece(const PagedParams& p, const Piece& e, 
   }
 
   // the four waves' (max, sum, O), through their own buffers
-  const float l_tot = half_sum(l_run);
+  const float l_tot = half_sum(l_run.sum);
   if (hh == 0) {
     S.m[w][c] = m2;
     S.l[w][c] = l_tot;

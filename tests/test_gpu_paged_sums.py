@@ -2,7 +2,9 @@
 one score, so that every weight and every sum is rounded the same way.
 
 Tolerances (u = 2^-24).  A weight: its score is one exact product times scale log2(e) less the maximum, 2 u of at most 12
-in log2 units, with the exponential's own step 2e-6; two bf16 parts 2^-17, one 2^-9 (where it rounds; 2^-8 allowed)."""
+in log2 units, with the exponential's own step 2e-6; two bf16 parts 2^-17, one 2^-8 (half a step of 8 bits, at a power
+of two).  The sum of the weights: chains of 8 and two more additions in a tile, 10 u, then compensated, 2 u: 8e-7.  LSE: a
+weight's and the sum's, 3e-6, and the two roundings and log2's step at |lse| below 20, 4 u |lse| = 5e-6."""
 import pytest
 import torch
 
@@ -51,9 +53,31 @@ def half_step(x):
 @pytest.mark.parametrize("T,hq,keys", [(1, 32, 512), (1, 32, 16384), (8, 4, 1024), (8, 4, 20480), (1, 7, 4096)])
 @pytest.mark.parametrize("d", [64, 128])
 def test_weights_of_few_rows_are_not_rounded_to_bf16(gpu, T, hq, keys, d):
-    """Values 1 .. 2 behind a sink of value 0: a weight rounded to bf16 shows in full, by up to 2^-9 of the result.  The
+    """Values 1 .. 2 behind a sink of value 0: a weight rounded to bf16 shows in full, by up to 2^-8 of the result.  The
     products' sums: 16,384 keys in chains of 16 keys a step, 1,280 steps at most, 4e-5 at half a step each on a sum that
     grows evenly."""
     out, _, want, _, size = sink(BF, d, keys, T, hq, 1 + torch.arange(d, device="cuda")[None] / d, 0.0)
     over = (out.double() - want).abs() - (2.0 ** -17 + 2e-6 + 4e-5) * size - half_step(want)
     assert over.max() <= 0, over.max()
+
+
+# row blocks that walk all keys (512 of 128 rows), and such as are cut; sequences of few rows
+LONG = [(BF, 64, 1 << 17, 1024, 64), (BF, 128, 1 << 20, 1024, 64), (BF, 128, 1 << 20, 1, 32), (BF, 128, 1 << 17, 20, 64),
+        (F32, 64, 1 << 17, 1024, 64), (F32, 128, 1 << 17, 1024, 64), (F32, 64, 1 << 20, 8, 8), (F32, 128, 1 << 18, 100, 4)]
+
+
+def normal(d, keys):
+    return 1 + torch.randn(keys, d, generator=torch.Generator(device="cuda").manual_seed(d), device="cuda")
+
+
+@pytest.mark.parametrize("case", LONG, ids=str)
+def test_sum_of_many_weights(gpu, case):
+    dt, d, keys, T, hq = case
+    out, lse, want, want_lse, size = sink(dt, d, keys, T, hq, normal(d, keys))
+    assert ((lse.double() - want_lse).abs() <= 3e-6 + 4 * 2.0 ** -24 * want_lse.abs()).all()
+    if dt is BF:
+        # O's sums: 16 keys a step, 2^16 steps at 1,048,576 keys, half a step of rounding in each on a sum that grows
+        # evenly: u 2^16 / 2 = 2e-3, of one sign only where the values are equal: here they
+            # differ, and the steps' roundings are as a walk, u 2^8 = 2e-5
+        over = (out.double() - want).abs() - (2.0 ** -8 + 1e-4) * size - half_step(want)
+        assert over.max() <= 0, over.max()
