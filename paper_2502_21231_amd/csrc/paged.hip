@@ -722,7 +722,15 @@ struct FewOps<float, D> {
   };
   static __device__ __forceinline__ void put(P& p, int, int r, float v) { p.x[r] = v; }
   __device__ __forceinline__ void values(const float* V, const P& p, f32x16 (&o)[DB]) const {
-    col_products<D>(reinterpret_cast<const char*>(V), cbase, p.x, o);
+    // a tile's products have sums of their own, which are one addition to O's: two keys a step would be as many roundings
+    // as keys / 2, all one way over values of one size (131,072 keys of one value, in one chain: 1.9e-3 of O; so 6e-5, for
+    // 1 to 2 % of the time of prompts, one of 4,096, 32/8 heads 1.12 -> 1.14 ms)
+    f32x16 t[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) t[db] = f32x16{};
+    col_products<D>(reinterpret_cast<const char*>(V), cbase, p.x, t);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] += t[db];
   }
   static __device__ __forceinline__ void put_rows(float* K, float*, int lane, const f32x16 (&o)[DB]) {
     put_acc<D>(reinterpret_cast<char*>(K), lane, o);
@@ -746,10 +754,14 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   const Ops ops(lane);
   const int qrow = w * 32 + c;
   const bool qvalid = qrow < e.rows;
-  const Row row = row_of(p, e, (uint32_t)(e.rb * BM + (qvalid ? qrow : 0)));
+  const uint32_t r_lane = (uint32_t)(e.rb * BM + (qvalid ? qrow : 0));
   typename Ops::Q qf[Ops::NQ];
-  Ops::load(qf, static_cast<const float*>(p.q) + row.at * D, hh);
-  const int lim_base = seen_by(p, e, row.qi) - hh * 4;
+  int lim_base;
+  {
+    const Row r = row_of(p, e, r_lane);
+    Ops::load(qf, static_cast<const float*>(p.q) + r.at * D, hh);
+    lim_base = seen_by(p, e, r.qi) - hh * 4;
+  }
   const int full = seen_by(p, e, (int)((uint32_t)(e.rb * BM) / (uint32_t)p.group));
   const int n_full = __builtin_amdgcn_readfirstlane(full > 0 ? full / BN : 0);  // tiles that all rows see whole
   const int t0 = e.kb, n_tiles = e.kb + e.n, keys = e.lk;
@@ -836,6 +848,9 @@ __device__ __forceinline__ void tile_piece(const PagedParams& p, const Piece& e,
   const float l_tot = half_sum(l_run.sum);
   if (!qvalid) return;
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  uint32_t r1 = r_lane;
+  asm volatile("" : "+v"(r1));  // worked out again, as in the form of bf16
+  const Row row = row_of(p, e, r1);
   float* op = static_cast<float*>(p.o) + row.at * D;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {

@@ -81,3 +81,15 @@ def test_sum_of_many_weights(gpu, case):
             # differ, and the steps' roundings are as a walk, u 2^8 = 2e-5
         over = (out.double() - want).abs() - (2.0 ** -8 + 1e-4) * size - half_step(want)
         assert over.max() <= 0, over.max()
+
+
+@pytest.mark.parametrize("T,hq,d", [(1024, 64, 64), (1024, 64, 128), (300, 64, 64), (1, 16, 128)])
+@pytest.mark.parametrize("equal", [True, False])
+def test_float32_sums_of_many_products(gpu, T, hq, d, equal):
+    """Out.  Within a tile of 32 keys 16 steps from 0, 2 u each, and a weight's 3e-6: 5e-6.  Then one addition a tile to a
+    sum that grows evenly, u / 2 of its end each: in the tile form (head_dim 128, 512 row blocks) keys / 32 of them, in
+    the few form each of four waves has a fourth of the keys."""
+    keys = 1 << 17
+    out, _, want, _, size = sink(F32, d, keys, T, hq, torch.ones(1, d, device="cuda") if equal else normal(d, keys))
+    steps = keys / 32 / (1 if d == 128 and T == 1024 else 4)
+    assert ((out.double() - want).abs() <= (5e-6 + 2.0 ** -25 * steps) * size).all()
