@@ -1258,8 +1258,8 @@ bool paged_fits(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_k, int64_
   const PagedLayout L = paged_layout(d, num_seqs, max_seqlen_k);
   if (L.mode != kLine) return L.grid < (1 << 24);  // (a grid has less than 2^32 threads)
   const int64_t rows = d.total_q * (d.hq / d.hkv);
-  const int64_t places = d.dtype == BS_BF16 ? (rows / kTileBM + num_seqs) * (keys / kTileBN + 3)
-                                            : (rows / kFewBM + num_seqs) * (keys / 128 + 3);
+  const int64_t places = d.dtype == BS_BF16 ? paged_places(rows, num_seqs, keys, kTileBM, kTileBN)
+                                            : paged_places(rows, num_seqs, keys, kFewBM, 4 * few_keys<float, 64>());
   return places < INT32_MAX && places * d.hkv < int64_t(1) << 39;
 }
 

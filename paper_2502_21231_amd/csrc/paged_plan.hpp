@@ -10,7 +10,8 @@
 //   S(i) = floor(i (A + i B)),  A + B (2 i + 1) >= v(i) + 1 / BLK
 // a sum of the unrounded counts: S(i + 1) - S(i) >= floor(A + B (2 i + 1)) >= v(i), about one slot
 // more than needed on average.  The slots behind the v(i)-th are skipped.  The one row block of a
-// short segment has its v exactly.
+// short segment has its v exactly.  Where a segment has more queries than keys, its first row blocks see none: they
+// have a slot each, and i counts from the first block that may see a key.
 #pragma once
 
 #include <stdint.h>
@@ -47,15 +48,19 @@ BS_HD int32_t paged_blocks(const PagedSeg& s, int BM, int BLK, int32_t i) {
 // The slots of a segment.
 struct PagedCost {
   double a, b;
-  int32_t n;  // row blocks
+  int32_t n, none;  // row blocks, and how many of them, the first, are known to see no key
   // (a product of one rounding, so that every caller gets the same number)
-  BS_HD int32_t start(int32_t i) const { return (int32_t)(i * __builtin_fma((double)i, b, a)); }
+  BS_HD int32_t start(int32_t i) const {
+    const int32_t j = i - none;
+    return j <= 0 ? i : none + (int32_t)(j * __builtin_fma((double)j, b, a));
+  }
   // The row block that slot y of the segment belongs to.
   BS_HD int32_t find(int32_t y) const {
     if (n == 1) return 0;
-    double g = b > 0 ? (__builtin_sqrt(a * a + 4 * b * (double)y) - a) / (2 * b) : (double)y / a;
-    int32_t i = g < n ? (int32_t)g : n - 1;
-    while (i > 0 && start(i) > y) --i;
+    if (y < none) return y;
+    double g = b > 0 ? (__builtin_sqrt(a * a + 4 * b * (double)(y - none)) - a) / (2 * b) : (double)y / a;
+    int32_t i = none + g < n ? none + (int32_t)g : n - 1;
+    while (i > none && start(i) > y) --i;
     while (i + 1 < n && start(i + 1) <= y) ++i;
     return i;
   }
@@ -63,15 +68,26 @@ struct PagedCost {
 BS_HD PagedCost paged_cost(const PagedSeg& s, int BM, int BLK) {
   PagedCost c;
   c.n = paged_row_blocks(s, BM);
+  c.none = 0;
   c.b = 0;
   c.a = s.lk > BLK ? (s.lk + BLK - 1) / BLK : 1;
   if (s.causal && c.n > 1) {
     const double step = (double)BM / s.group / BLK;
-    const int32_t first = s.lk - s.lq + 1;
+    int32_t first = s.lk - s.lq + 1;  // keys of the first query
+    if (first < 1) {
+      c.none = (int32_t)((int64_t)(s.lq - s.lk) * s.group / BM);
+      first = 1;  // (of the query that sees one, and not before row block `none`)
+    }
     c.b = step * 0.5;
-    c.a = (double)((first > 0 ? first : 0) + BLK) / BLK + c.b;
+    c.a = (double)(first + BLK) / BLK + c.b;
   }
   return c;
+}
+
+// Slots of sequences of so many rows and at most so many keys each, at most: S(n) is n times at most
+// lk / BLK + 1 + 1 / BLK + 3 B, and B <= 1 (128 rows of as many queries, 64 keys).
+BS_HD int64_t paged_places(int64_t rows, int64_t seqs, int64_t keys, int BM, int BLK) {
+  return (rows / BM + seqs) * (keys / BLK + 5);
 }
 
 // Workgroups that run at a time (two per CU), the ranges of a line at most, and parts of a row block's keys at most.
