@@ -1,12 +1,12 @@
-"""Paged attention shared as a line, over more sequences than a workgroup has threads, one of them of more new tokens than
-keys.  Bounds as in test_gpu_paged.py."""
+"""Paged attention shared as a line, over more sequences than a workgroup has threads: sequences of several row blocks
+among many others, and one of more new tokens than keys.  Bounds as in test_gpu_paged.py."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2502_21231_amd import bs_attn as B
 from paper_2502_21231_amd import bs_qkv as Q
-from tests.test_gpu_paged import BF, F32, check
+from tests.test_gpu_paged import BF, F32, check, run_case
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +44,33 @@ def test_more_tokens_than_keys(gpu, dt, tokens, lk):
         for w, x in zip(want, ((p @ vv)[:, None], s.logsumexp(1)[None], (p @ vv.abs())[:, None])):
             (w[:, lo:lo + rows] if w is want[1] else w[lo:lo + rows])[:] = x.cpu().numpy()
     check(out[tokens - lk:], lse[:, tokens - lk:], want, lk + 1, dt)
+
+
+def many(seqs, chunks, keys, empty):
+    """Lengths of `seqs` sequences of one query each, every `empty`-th of none; {sequence: (new tokens, length)} of others."""
+    rng = np.random.default_rng(seqs)
+    lens = [int(x) for x in rng.integers(1, keys, seqs)]
+    new = [0 if i % empty == 3 else 1 for i in range(seqs)]
+    for b, (n, length) in chunks.items():
+        new[b], lens[b] = n, length
+    return lens, new
+
+
+# more than 256 sequences, so several per thread; chunks of several row blocks at a thread's first, middle and last one
+MANY = [
+    (300, {150: (250, 1500)}, 1100, 16, 8, 2, 128, BF),
+    (300, {0: (100, 100), 299: (130, 2100)}, 700, 16, 8, 1, 64, BF),
+    (1030, {517: (200, 3000), 518: (140, 90), 1029: (300, 1200)}, 60, 16, 2, 1, 64, BF),
+    (300, {151: (200, 1300)}, 1100, 16, 4, 2, 64, F32),
+    (300, {1: (33, 20), 298: (70, 1400)}, 300, 32, 6, 2, 128, F32),
+    (777, {400: (300, 1100), 402: (64, 64)}, 40, 16, 1, 1, 128, F32),
+]
+
+
+@pytest.mark.parametrize("case", MANY, ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunks_among_many_sequences(gpu, case, causal):
+    seqs, chunks, keys, page, hq, hkv, d, dt = case
+    lens, new = many(seqs, chunks, keys, 5)
+    assert dt is F32 or sum(new) + 2 <= 2 * seqs  # (bf16: the line's rule)
+    run_case(lens, new, page, hq, hkv, d, dt, causal=causal, pad=2, most=4000)
