@@ -106,7 +106,9 @@ size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32
  * j is visible to row i of n iff j <= i + kv_lens[b] - n, otherwise all are.  q [T, hq, head_dim]
  * contiguous; writes out [T, hq, head_dim] and lse [hq, T]; a row that sees no key gets out = 0,
  * lse = -inf.  Rows from cu_seqlens_q[num_seqs] on are left as they were.  What the pages hold behind
- * a sequence's last token is not looked at (it may be NaN).
+ * a sequence's last token is not looked at (it may be NaN). Among what is: a key of NaN gives NaN in out and
+ * lse of the rows that see it, and in no others; a value of NaN or infinity also gives NaN in out of rows that do not
+ * see its key but are worked on beside rows of their sequence that do (0 times it).
  *   - bf16: a sequence of more than 32 rows (queries x heads of a KV group) has its probabilities rounded to
  *     bf16 before their product with V, as in bs_attn_varlen_fwd; of up to 32 rows they are within 2^-17.  LSE
  *     is that of the unrounded ones.

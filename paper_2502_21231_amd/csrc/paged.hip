@@ -405,7 +405,8 @@ __device__ __forceinline__ Row row_of(const PagedParams& p, const Piece& e, uint
   x.at = ((int64_t)e.q_start + x.qi) * p.hq + x.head;
   return x;
 }
-__device__ __forceinline__ float lse_of(float m2, float l) { return l > 0.f ? (m2 + log2f(l)) * kLn2 : -INFINITY; }
+// (a NaN among the scores is one in the sum; -inf says that no key is seen)
+__device__ __forceinline__ float lse_of(float m2, float l) { return l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2; }
 // Keys that the row's query sees.
 __device__ __forceinline__ int seen_by(const PagedParams& p, const Piece& e, int qi) {
   return p.causal ? min(e.lk, qi + e.lk - e.lq + 1) : e.lk;
