@@ -20,11 +20,12 @@
 // paged_merge_kernel combines them.  Every workgroup lays out the line from the lengths itself: only
 // shapes are known on the host, so a captured call can be replayed with other lengths.
 //
-// Measured: 32 single queries over up to 8K keys, 64/8 heads of 128, bf16: 80 us, 5.4 TB/s (the merge 4 of it); 256 over
-// up to 4K, 32/8: 307 us, 6.1 TB/s; one over 3K, 32/8: 12 us, two launches that leave the chip empty.  8 chunks
-// of up to 1,024 queries over up to 16K keys, 64/8: 1.53 to 1.60 ms, 1,000 to 1,040 TFLOP/s of visible pairs, within
-// 4 % of the contiguous forward.  A chunk of 509 among 16 single queries over 8K, 48/8: 92 us, of which the keys' bytes
-// alone are 56.  float32, 3 x up to 200 queries over 700, 8/4 heads of 64: 18 us, a chain of key blocks and a merge.
+// Measured: 32 single queries over up to 8K keys, 64/8 heads of 128, bf16: 80 us, 5.4 TB/s (the merge 4 of it), float32,
+// 32/8: 173 us, 5.3 TB/s; 256 over up to 4K, 32/8, bf16: 302 us, 6.0 TB/s; one over 3K, 32/8: 12 us, two launches that
+// leave the chip empty.  8 chunks of up to 1,024 queries over up to 16K keys, 64/8: 1.53 to 1.60 ms, 1,000 to 1,040
+// TFLOP/s of visible pairs, within 4 % of the contiguous forward.  A chunk of 509 among 16 single queries over 8K, 48/8:
+// 93 us, of which the keys' bytes alone are 56.  float32, 3 x up to 200 queries over 700, 8/4 heads of 64: 18 us, a chain
+// of key blocks and a merge.
 //
 // Pages.  A wave copies 16 neighbouring keys at a time, which lie in one page (page_size is a multiple
 // of 16), so a page's place is scalar work, one number of the table per 16 keys, read a tile ahead.
@@ -72,7 +73,7 @@ struct PagedParams {
   int32_t parts;      // items: whether row blocks may be shared (> 1)
   int32_t bm;         // rows of a piece's room in stat and part
   int64_t total_q;
-  int32_t num_seqs, max_pages, page_shift, max_len;
+  int32_t num_seqs, page_shift, max_len;  // max_len: no more than the table holds
   int32_t hq, hkv, group;
   int32_t causal;
   float scale_log2;
@@ -351,7 +352,7 @@ __device__ __forceinline__ bool item_piece(const PagedParams& p, const PagedLds&
   c.rb = __builtin_amdgcn_readfirstlane(nrb - 1 - back);
   c.v = __builtin_amdgcn_readfirstlane(paged_blocks(s, f.bm, f.blk, c.rb));
   c.rows = min((int)(c.lq * p.group - c.rb * f.bm), f.bm);
-  c.pieces = min(max_parts, c.v);  // (up to 4 blocks in a part at least: 3 x 200 over 700, float32, 31 us instead of 21)
+  c.pieces = min(max_parts, c.v);  // (a part may be one block; with four at least 3 x 200 over 700, float32, took 31 us for 21)
   if (part >= c.pieces) return false;
   c.kb = __builtin_amdgcn_readfirstlane(part * c.v / c.pieces);
   c.n = __builtin_amdgcn_readfirstlane((part + 1) * c.v / c.pieces) - c.kb;
@@ -725,7 +726,7 @@ struct FewOps<float, D> {
   __device__ __forceinline__ void values(const float* V, const P& p, f32x16 (&o)[DB]) const {
     // a tile's products have sums of their own, which are one addition to O's: two keys a step would be as many roundings
     // as keys / 2, all one way over values of one size (131,072 keys of one value, in one chain: 1.9e-3 of O; so 6e-5, for
-    // 1 to 2 % of the time of prompts, one of 4,096, 32/8 heads 1.12 -> 1.14 ms)
+    // 1 to 4 % of the time of prompts, one of 4,096, 32/8 heads 1.12 -> 1.14 ms, 64 x up to 60, head_dim 64, 49 -> 51 us)
     f32x16 t[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) t[db] = f32x16{};
@@ -1218,10 +1219,10 @@ PagedLayout paged_layout(const bs_dims& d, int32_t num_seqs, int32_t max_seqlen_
   else if (bf) L.mode = few && d.total_q <= 2 * seqs ? kLine : kTileItems;
   else L.mode = line32 ? kLine : kFewItems;
   // Float32 tiles, where those fill the chip.  At head_dim 128 the few form has a CU's LDS to itself, and all it does
-  // before and after its products counts: 36 prompts of up to 154 tokens, 32/4 heads 180 -> 97 us, one of 4,096, 32/8
-  // 1.25 -> 1.13 ms.  A single query's chain of many keys is four times as long, though (a chunk of 2,000 among 32
+  // before and after its products counts: 36 prompts of up to 154 tokens, 32/4 heads 160 -> 76 us, one of 4,096, 32/8
+  // 1.27 -> 1.14 ms.  A single query's chain of many keys is four times as long, though (a chunk of 2,000 among 32
   // single queries over 4K, 32/8: 818 us without tiles, 1,015 with).  At head_dim 64 two workgroups of the few form
-  // share a CU, and tiles are ahead over few keys only: 36 x 154 80 -> 54 us, but 64 x 60 over 500 49 -> 63.
+  // share a CU, and tiles are ahead over few keys only: 36 x 154 73 -> 45 us, 64 x 60 over 200 69 -> 51, but over 500 49 -> 63.
   const bool short_chains = d.head_dim == 64 ? max_seqlen_k <= 256
                                              : max_seqlen_k <= 2048 || rows >= 8 * kTileBM * seqs;
   if (!bf && seqs > 0 && !few && blocks(kTileBM) >= kPagedSlots && short_chains) L.mode = kTileItems;
@@ -1292,7 +1293,6 @@ hipError_t launch_paged_fwd(const bs_dims& d, const void* q, const bs_paged_cach
   p.bm = W.bm;
   p.total_q = d.total_q;
   p.num_seqs = num_seqs;
-  p.max_pages = C.max_pages;
   p.page_shift = __builtin_ctz((unsigned)C.page_size);
   const int64_t room = (int64_t)C.max_pages * C.page_size;
   p.max_len = (int32_t)(max_seqlen_k < room ? max_seqlen_k : room);
