@@ -29,7 +29,9 @@ extern "C" {
  *     a' = a cos - b sin,  b' = b cos + a sin;
  *   pairs are elements (i, i + rot_dim / 2), or (2i, 2i + 1) with interleaved != 0; the other
  *   head_dim - rot_dim elements are not rotated.
- * The angle is formed and reduced in float64 (for |t| < 2^31 it is within 1e-6 of t inv_freq[i]). */
+ * The angle is formed and reduced in float64 (for |t| < 2^31 it is within 1e-6 of t inv_freq[i]), then rounded to a
+ * float32 part of a turn; sine, cosine and the root are float32 functions of it (float32 results within some 6e-6 of
+ * a head's largest element, 1.3e-7 in the norm of the whole). */
 typedef struct {
   const float* inv_freq;  /* float32 [rot_dim / 2] on the device; NULL with rot_dim == 0 */
   int32_t rot_dim;        /* 0 (no rotation) .. head_dim, a multiple of 16 */
@@ -107,8 +109,8 @@ size_t bs_attn_paged_workspace_size(const bs_dims* dims, int32_t num_seqs, int32
  * contiguous; writes out [T, hq, head_dim] and lse [hq, T]; a row that sees no key gets out = 0,
  * lse = -inf.  Rows from cu_seqlens_q[num_seqs] on are left as they were.  What the pages hold behind
  * a sequence's last token is not looked at (it may be NaN). Among what is: a key of NaN gives NaN in out and
- * lse of the rows that see it, and in no others; a value of NaN or infinity also gives NaN in out of rows that do not
- * see its key but are worked on beside rows of their sequence that do (0 times it).
+ * lse of the rows that see it, and in no others; a value of NaN or infinity may also
+ * give NaN in out of rows shortly before its token, which do not see it (0 times it).
  *   - bf16: a sequence of more than 32 rows (queries x heads of a KV group) has its probabilities rounded to
  *     bf16 before their product with V, as in bs_attn_varlen_fwd; of up to 32 rows they are within 2^-17.  LSE
  *     is that of the unrounded ones.
